@@ -390,6 +390,148 @@ ca_status ca_packed_chunk_attention(const ca_problem* p, const uint16_t* q,
                                     void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * 5. The serving step around the paged cache: pages and slots for the new
+ *    tokens, rotary positions and the cache write, attention of one new
+ *    token per request.  The calls share the pool and page-table layouts of
+ *    the file header with the chunk path, so a cache that they fill is read
+ *    by sections 1 to 4 and the other way round.
+ *
+ *    No length is needed on the host: every length, count and page id is read
+ *    from device memory when the kernels run, so a captured graph of a step
+ *    can be replayed while its requests grow, and nothing depends on a value
+ *    the host has not seen.  What the host cannot check the kernels bound: a
+ *    length, table entry, page id or slot that is out of range is never used
+ *    as an address (what happens instead is said at each call).
+ * ---------------------------------------------------------------------- */
+typedef struct ca_cache {
+  int32_t batch;             /* B >= 1: requests, the rows of page_table        */
+  int32_t num_q_heads;       /* Hq, B * Hq < 2^31                               */
+  int32_t num_kv_heads;      /* Hkv, divides Hq                                 */
+  int32_t head_dim;          /* D, 64 or 128                                    */
+  int32_t page_size;         /* tokens per page; must be 64                     */
+  int32_t max_kv_blocks;     /* row stride of page_table, 1 .. 16384            */
+  int32_t num_pages;         /* pages of k_pool and v_pool, >= 1                */
+  int32_t v_layout;          /* CA_V_TOKEN_MAJOR or CA_V_TRANSPOSED             */
+} ca_cache;
+
+/* Host-only validation; every entry point of this section performs it first.
+ * group_size > 0 is checked against Hq / Hkv as by ca_check_problem. */
+ca_status ca_check_cache(const ca_cache* c, int32_t group_size);
+
+/* 5a. Pages and slots.  free_pages int32 [free_capacity] is a stack: its first
+ *    free_count[0] entries are the pages that no request holds, the last of
+ *    them is taken first.  seq_len int32 [B] are the requests' cached tokens.
+ *
+ *    ca_assign_slots: request b adds new_len[b] >= 0 tokens at positions
+ *    seq_len[b], seq_len[b] + 1, ..  The step's tokens are packed request by
+ *    request: rows token_indptr[b] .. token_indptr[b+1] of num_tokens rows, the
+ *    rest is padding.  A block that opens (position a multiple of 64) takes one
+ *    free page for every KV head, in the order of the requests, then the
+ *    blocks, then the heads; page_table gets the ids.
+ *      slot_map int64 [num_tokens, Hkv]: page * 64 + position % 64, the row of
+ *        a token-major pool seen as [P * 64, D]; -1 where nothing is to be
+ *        written (padding, a refused request, a page id outside the pool);
+ *      positions int32 [num_tokens]: the tokens' positions, 0 where the
+ *        request was refused and in the padding;
+ *      token_indptr int32 [B + 1]: the prefix sum of max(new_len, 0), at most
+ *        num_tokens;
+ *      granted int32 [B]: new_len[b], or 0 for a refused request;
+ *      seq_len_out int32 [B]: seq_len + granted;
+ *      free_count_out int32 [1]: the free pages left.
+ *    A request is refused (it keeps its length and pages; its token rows stay
+ *    its own) when new_len or seq_len is negative, when it would need more
+ *    than max_kv_blocks blocks, when its rows end after num_tokens, and when
+ *    the pages it needs and those needed by the requests before it are more
+ *    than there are: from the first request that the pages do not reach on,
+ *    requests that need none are still served.
+ *
+ *    ca_release_pages: the requests with release[b] != 0 end: their pages are
+ *    put behind the free ones, in the order of the requests, then the blocks,
+ *    then the heads, and their length becomes 0.  A request whose length is
+ *    out of range or whose pages do not fit in free_capacity keeps them; the
+ *    requests after the first that do not fit as well, if they hold any.
+ *
+ *    seq_len_out may be seq_len and free_count_out may be free_count (the step
+ *    is then in place, and one workgroup does it all, which is enough for
+ *    decode steps); no other buffers may overlap.  num_tokens may be 0.
+ * ---------------------------------------------------------------------- */
+ca_status ca_assign_slots(const ca_cache* c, const int32_t* new_len, int32_t num_tokens,
+                          const int32_t* seq_len, int32_t* page_table,
+                          const int32_t* free_pages, int32_t free_capacity,
+                          const int32_t* free_count, int64_t* slot_map, int32_t* positions,
+                          int32_t* token_indptr, int32_t* granted, int32_t* seq_len_out,
+                          int32_t* free_count_out, void* stream);
+
+ca_status ca_release_pages(const ca_cache* c, const int32_t* release, const int32_t* seq_len,
+                           const int32_t* page_table, int32_t* free_pages,
+                           int32_t free_capacity, const int32_t* free_count,
+                           int32_t* seq_len_out, int32_t* free_count_out, void* stream);
+
+/* 5b. Rotary positions and the cache write, in one pass over the step's
+ *    queries, keys and values.  Pair i of a head (i < rot_dim / 2) turns by
+ *        angle = positions[axis(i), t] * inv_freq[i]
+ *        (a, b) -> (a cos - b sin, b cos + a sin)
+ *    with (a, b) = elements (i, i + rot_dim / 2), or (2i, 2i + 1) with
+ *    interleaved; elements from rot_dim on are left as they are.  The angle is
+ *    formed in double precision and reduced to a part of a turn there, so
+ *    far positions keep theirs; cosine, sine and the rotation are fp32, and
+ *    the result is rounded once to bf16.
+ *    Several axes (time, height, width of an image's or video's tokens):
+ *    positions int32 [num_axes, num_tokens], and pair_axis_host names every
+ *    pair's axis (NULL: axis 0), so sections and interleaved assignments are
+ *    both just a list.
+ *    q [num_tokens, Hq, D], k and v [num_tokens, Hkv, D] may be parts of a
+ *    fused projection's output: token t starts at q + t * q_stride (elements,
+ *    a multiple of 8; heads of a token are contiguous).  The rotated queries
+ *    go to q_out [num_tokens, Hq, D] (dense; q_out may be q if q is dense),
+ *    rotated keys and the values to slot_map's places in k_pool and v_pool.
+ *    A slot outside [0, num_pages * 64) writes nothing; the slots of one call
+ *    must differ from each other.  num_tokens = 0 does nothing.  rot_dim = 0
+ *    rotates nothing.  batch and max_kv_blocks of the cache are not used.
+ * ---------------------------------------------------------------------- */
+typedef struct ca_rotary {
+  int32_t rot_dim;            /* rotated elements of a head: 0 .. D, a multiple of 16 */
+  int32_t interleaved;        /* 0: pairs (i, i + rot_dim/2); 1: pairs (2i, 2i + 1)   */
+  int32_t num_axes;           /* 1 .. 4                                               */
+  const int32_t* pair_axis_host; /* HOST [rot_dim / 2], in [0, num_axes); may be NULL */
+  const float* inv_freq;      /* DEVICE [rot_dim / 2], radians per position           */
+} ca_rotary;
+
+ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_tokens,
+                           const uint16_t* q, int64_t q_stride, const uint16_t* k,
+                           int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                           const int32_t* positions, const int64_t* slot_map, uint16_t* q_out,
+                           uint16_t* k_pool, uint16_t* v_pool, void* stream);
+
+/* 5c. Attention of one new token per request over its cache (the token's own
+ *    key and value are in the cache already).
+ *    q bf16 [B, Hq, D]; out bf16 [B, Hq, D]; lse fp32 [B, Hq] (natural log, may
+ *    be NULL); kv_len int32 [B], DEVICE only: request b attends to the keys at
+ *    positions < kv_len[b] of every block 0 .. ceil(kv_len[b] / 64) - 1, or,
+ *    with kv_indptr and kv_indices (both or neither), of the blocks in
+ *    T[b, h / group_size] (the CSR tables of section 2, built from
+ *    a problem with the same B and group_size).  group_size must divide
+ *    Hq / Hkv; 0 stands for Hq / Hkv.
+ *        out = softmax(sm_scale * q.k) . v     (bf16 MFMA, fp32 softmax)
+ *    A request that sees no key (kv_len 0, an empty table row) gets out = 0,
+ *    lse = -inf; a score of NaN or +inf gives out = NaN, lse = -inf, as in
+ *    section 3.  A value that is not finite makes the elements of out that it
+ *    reaches not finite.  The keys past kv_len may hold anything, NaN included.
+ *    kv_len is taken as 0 below 0 and as 64 * max_kv_blocks above it; blocks
+ *    whose table entry or page id is out of range add no keys.
+ *    Workspace: ca_decode_workspace_bytes(c, group_size) bytes, 16-byte aligned,
+ *    whatever it holds; calls that may overlap must not share one.
+ * ---------------------------------------------------------------------- */
+size_t ca_decode_workspace_bytes(const ca_cache* c, int32_t group_size);
+
+ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16_t* k_pool,
+                              const uint16_t* v_pool, const int32_t* page_table,
+                              const int32_t* kv_len, const int32_t* kv_indptr,
+                              const int32_t* kv_indices, int32_t group_size, float sm_scale,
+                              uint16_t* out, float* lse, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/* ------------------------------------------------------------------------
  * Debug helper: synchronises `stream`, copies the tables to the host and
  * checks kv_indptr[0] == 0, non-decreasing row bounds within capacity,
  * entries strictly ascending and < nKB_b, and (if require_chunk_open) that

@@ -20,6 +20,9 @@ It is a plain, slow, float64 restatement of what the paper defines:
   same softmax per (head, Q-block) mask row without any union, the block-
   sparse execution the paper compares against (Sec. 4.4).
 
+* ``serving``    -- the steps between the chunks: pages and slots for new tokens,
+  rotary positions, attention of one new token per request.
+
 Parity status of each function is stated in its docstring; every function is
 pinned by ``tests/test_oracle.py`` against properties that the paper or the
 mathematics fix.
@@ -34,3 +37,4 @@ from .tables import unpack_masks, block_tables, tables_to_csr, union_densities  
 from .attention import (  # noqa: F401
     gather_selected, attention_rows, chunk_attention, dense_tables, block_sparse_attention,
 )
+from . import serving  # noqa: F401

@@ -11,6 +11,8 @@ from .binding import (  # noqa: F401
     build_block_sparse_tables, block_sparse_chunk_attention, gather_selected_pages,
     packed_chunk_attention, estimate_masks_threshold, select_blocks_threshold, estimate_tables,
     build_block_tables_noalloc, check_tables_host,
+    Cache, Rotary, check_cache, assign_slots, release_pages, rotary_append,
+    decode_workspace_bytes, decode_attention,
     EXPORTED,
     LIB_PATH,
     DEBUG_LIB_PATH,

@@ -32,6 +32,8 @@ EXPORTED = (
     "ca_block_sparse_chunk_attention", "ca_gather_selected_pages", "ca_packed_chunk_attention",
     "ca_select_blocks_threshold", "ca_estimate_masks_threshold", "ca_estimate_tables",
     "ca_build_block_tables_noalloc", "ca_check_tables_host",
+    "ca_check_cache", "ca_assign_slots", "ca_release_pages", "ca_rotary_append",
+    "ca_decode_workspace_bytes", "ca_decode_attention",
 )
 
 
@@ -48,6 +50,29 @@ class CAProblem(ctypes.Structure):
         ("cached_len_host", _c_i32p),
         ("cached_len", ctypes.c_void_p),
         ("v_layout", ctypes.c_int32),
+    ]
+
+
+class CACache(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("max_kv_blocks", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("v_layout", ctypes.c_int32),
+    ]
+
+
+class CARotary(ctypes.Structure):
+    _fields_ = [
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("num_axes", ctypes.c_int32),
+        ("pair_axis_host", _c_i32p),
+        ("inv_freq", ctypes.c_void_p),
     ]
 
 
@@ -81,6 +106,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     P = ctypes.POINTER(CAProblem)
     vp, i32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
     i64 = ctypes.c_int64
+    C, RO = ctypes.POINTER(CACache), ctypes.POINTER(CARotary)
     sig = {
         "ca_abi_version": ([], ctypes.c_int),
         "ca_status_string": ([ctypes.c_int], ctypes.c_char_p),
@@ -114,6 +140,15 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
                                      ctypes.c_int),
         "ca_packed_chunk_attention": ([P, vp, vp, vp, vp, vp, i32, f32, i32, i64, vp, vp, vp,
                                        sz, vp], ctypes.c_int),
+        "ca_check_cache": ([C, i32], ctypes.c_int),
+        "ca_assign_slots": ([C, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp],
+                            ctypes.c_int),
+        "ca_release_pages": ([C, vp, vp, vp, vp, i32, vp, vp, vp, vp], ctypes.c_int),
+        "ca_rotary_append": ([C, RO, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp],
+                             ctypes.c_int),
+        "ca_decode_workspace_bytes": ([C, i32], sz),
+        "ca_decode_attention": ([C, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp],
+                                ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -546,3 +581,189 @@ def validate_tables(p: Problem, group_size: int, tables, require_chunk_open: boo
                     stream=None) -> None:
     _check(load().ca_validate_tables(p.ref, group_size, _ptr(tables[0]), _ptr(tables[1]),
                                      int(require_chunk_open), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# the serving step around the paged cache
+# ---------------------------------------------------------------------------
+class Cache:
+    """Sizes of a paged cache and of the requests that it serves (ca_cache)."""
+
+    def __init__(self, batch: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
+                 max_kv_blocks: int, num_pages: int, page_size: int = 64,
+                 v_layout: int = V_TOKEN_MAJOR):
+        self.batch, self.num_q_heads, self.num_kv_heads = batch, num_q_heads, num_kv_heads
+        self.head_dim, self.page_size = head_dim, page_size
+        self.max_kv_blocks, self.num_pages, self.v_layout = max_kv_blocks, num_pages, v_layout
+        self.c = CACache(batch, num_q_heads, num_kv_heads, head_dim, page_size, max_kv_blocks,
+                         num_pages, v_layout)
+        self.ref = ctypes.byref(self.c)
+        self._table = (batch, num_kv_heads, max_kv_blocks)
+        self._k_pool = (num_pages, page_size, head_dim)
+        self._v_pool = (num_pages, head_dim, page_size) if v_layout == V_TRANSPOSED else self._k_pool
+
+
+class Rotary:
+    """How positions turn queries and keys (ca_rotary).
+
+    ``inv_freq`` float32 ``[rot_dim / 2]`` on the GPU (None: no rotation);
+    ``pair_axis``: the axis of every pair when positions have several (None:
+    all axis 0)."""
+
+    def __init__(self, inv_freq: Optional[torch.Tensor], interleaved: bool = False,
+                 num_axes: int = 1, pair_axis: Optional[Sequence[int]] = None):
+        pairs = 0 if inv_freq is None else inv_freq.numel()
+        if pairs and inv_freq.dtype != torch.float32:
+            raise ValueError("inv_freq must be float32")
+        if pair_axis is not None and len(pair_axis) != pairs:
+            raise ValueError(f"pair_axis names {len(pair_axis)} axes for {pairs} pairs")
+        self.num_axes, self.inv_freq = num_axes, inv_freq
+        self._axes = (ctypes.c_int32 * pairs)(*pair_axis) if pair_axis is not None else None
+        self.c = CARotary(2 * pairs, int(interleaved), num_axes,
+                          ctypes.cast(self._axes, _c_i32p) if self._axes is not None else None,
+                          _ptr(inv_freq) if pairs else None)
+        self.ref = ctypes.byref(self.c)
+
+
+def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape, device: torch.device):
+    """The address of an argument of the serving step; its type, shape and place are checked,
+    since the kernels take them from the cache's sizes."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _here(t: torch.Tensor) -> torch.device:
+    """The device of a call: the current one, whose stream the call is enqueued on."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {t.device}, but the current device is "
+                         f"{'cuda:%d' % torch.cuda.current_device() if torch.cuda.is_available() else 'none'}")
+    return t.device
+
+
+def check_cache(c: Cache, group_size: int = 0) -> None:
+    _check(load().ca_check_cache(c.ref, group_size))
+
+
+def assign_slots(c: Cache, new_len: torch.Tensor, num_tokens: int, seq_len: torch.Tensor,
+                 page_table: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                 bufs: Optional[dict] = None, stream=None) -> dict:
+    """Pages and slots for the tokens that every request adds; page_table is written.
+
+    Returns ``bufs`` (made where missing): slot_map int64 [num_tokens, Hkv], and int32
+    positions [num_tokens], token_indptr [B + 1], granted [B], seq_len [B] and
+    free_count [1] after the step; the last two may be the inputs themselves."""
+    dev, i32, B = _here(new_len), torch.int32, c.batch
+    b = bufs if bufs is not None else {}
+    for key, shape, dtype in (("slot_map", (num_tokens, c.num_kv_heads), torch.int64),
+                              ("positions", (num_tokens,), i32), ("token_indptr", (B + 1,), i32),
+                              ("granted", (B,), i32), ("seq_len", (B,), i32),
+                              ("free_count", (1,), i32)):
+        if key not in b:
+            b[key] = torch.empty(shape, dtype=dtype, device=dev)
+    _check(load().ca_assign_slots(
+        c.ref, _need("new_len", new_len, i32, (B,), dev), num_tokens,
+        _need("seq_len", seq_len, i32, (B,), dev), _need("page_table", page_table, i32, c._table, dev),
+        _need("free_pages", free_pages, i32, (free_pages.numel(),), dev), free_pages.numel(),
+        _need("free_count", free_count, i32, (1,), dev),
+        _need("slot_map", b["slot_map"], torch.int64, (num_tokens, c.num_kv_heads), dev),
+        _need("positions", b["positions"], i32, (num_tokens,), dev),
+        _need("token_indptr", b["token_indptr"], i32, (B + 1,), dev),
+        _need("granted", b["granted"], i32, (B,), dev), _need("seq_len", b["seq_len"], i32, (B,), dev),
+        _need("free_count", b["free_count"], i32, (1,), dev), _stream(stream)))
+    return b
+
+
+def release_pages(c: Cache, release: torch.Tensor, seq_len: torch.Tensor,
+                  page_table: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None):
+    """Ends the requests with release != 0: their pages go behind the free ones in free_pages.
+    Returns (seq_len, free_count) after it, which may be the inputs themselves (``out``)."""
+    dev, i32, B = _here(release), torch.int32, c.batch
+    if out is None:
+        out = (torch.empty_like(seq_len), torch.empty_like(free_count))
+    _check(load().ca_release_pages(
+        c.ref, _need("release", release, i32, (B,), dev), _need("seq_len", seq_len, i32, (B,), dev),
+        _need("page_table", page_table, i32, c._table, dev),
+        _need("free_pages", free_pages, i32, (free_pages.numel(),), dev), free_pages.numel(),
+        _need("free_count", free_count, i32, (1,), dev), _need("seq_len", out[0], i32, (B,), dev),
+        _need("free_count", out[1], i32, (1,), dev), _stream(stream)))
+    return out
+
+
+def _rows(name: str, t: torch.Tensor, heads: int, dim: int, rows: int, device: torch.device):
+    """Address and token stride of [rows, heads, dim] whose tokens may lie apart."""
+    if (t.dtype != torch.bfloat16 or t.shape != (rows, heads, dim) or t.device != device
+            or (rows and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)))):
+        raise ValueError(f"{name} must be a bfloat16 tensor {[rows, heads, dim]} on {device} with "
+                         f"contiguous heads, got {t.dtype} {list(t.shape)} on {t.device}, "
+                         f"strides {t.stride()}")
+    return t.data_ptr(), t.stride(0) if rows > 1 else heads * dim
+
+
+def rotary_append(c: Cache, r: Rotary, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                  positions: torch.Tensor, slot_map: torch.Tensor,
+                  kv_pool: Tuple[torch.Tensor, torch.Tensor], out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """Rotates q [T, Hq, D] and k [T, Hkv, D] by their positions ([T], or [axes, T]) and writes
+    keys and values to slot_map's places in the pools; returns the rotated queries.  q, k and v
+    may be parts of one tensor (a token's heads together, tokens apart)."""
+    dev, bf = _here(q), torch.bfloat16
+    T, Hq, Hkv, D = q.shape[0], c.num_q_heads, c.num_kv_heads, c.head_dim
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=bf, device=dev)
+    qp, qs = _rows("q", q, Hq, D, T, dev)
+    kp, ks = _rows("k", k, Hkv, D, T, dev)
+    vp, vs = _rows("v", v, Hkv, D, T, dev)
+    place = positions.shape if positions.dim() == 1 and r.num_axes == 1 else (r.num_axes, T)
+    if place[-1] != T:
+        raise ValueError(f"positions {list(positions.shape)} for {T} tokens")
+    if r.inv_freq is not None and r.inv_freq.device != dev:
+        raise ValueError(f"inv_freq on {r.inv_freq.device}, the tokens on {dev}")
+    _check(load().ca_rotary_append(
+        c.ref, r.ref, T, qp, qs, kp, ks, vp, vs,
+        _need("positions", positions, torch.int32, place, dev),
+        _need("slot_map", slot_map, torch.int64, (T, Hkv), dev), _need("out", out, bf, (T, Hq, D), dev),
+        _need("k_pool", kv_pool[0], bf, c._k_pool, dev), _need("v_pool", kv_pool[1], bf, c._v_pool, dev),
+        _stream(stream)))
+    return out
+
+
+def decode_workspace_bytes(c: Cache, group_size: int = 0) -> int:
+    return load().ca_decode_workspace_bytes(c.ref, group_size)
+
+
+def decode_attention(c: Cache, q: torch.Tensor, kv_pool: Tuple[torch.Tensor, torch.Tensor],
+                     page_table: torch.Tensor, kv_len: torch.Tensor, sm_scale: float,
+                     tables: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+                     group_size: int = 0, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                     stream=None):
+    """Attention of one new token per request, q [B, Hq, D], over its kv_len[b] cached tokens, or
+    over the blocks that ``tables`` (kv_indptr, kv_indices; one row per group of group_size heads,
+    0: all heads of a KV head) list; returns (out bf16, lse fp32 or None)."""
+    dev, bf, i32 = _here(q), torch.bfloat16, torch.int32
+    shape = (c.batch, c.num_q_heads, c.head_dim)
+    if out is None:
+        out = torch.empty(shape, dtype=bf, device=dev)
+    if ws is None:
+        n = decode_workspace_bytes(c, group_size)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous on {dev}")
+    indptr = indices = None
+    if tables is not None:
+        check_cache(c, group_size)
+        rows = c.batch * (c.num_q_heads // (group_size or c.num_q_heads // c.num_kv_heads))
+        indptr = _need("kv_indptr", tables[0], i32, (rows + 1,), dev)
+        indices = _need("kv_indices", tables[1], i32, (rows * c.max_kv_blocks,), dev)
+    _check(load().ca_decode_attention(
+        c.ref, _need("q", q, bf, shape, dev), _need("k_pool", kv_pool[0], bf, c._k_pool, dev),
+        _need("v_pool", kv_pool[1], bf, c._v_pool, dev),
+        _need("page_table", page_table, i32, c._table, dev),
+        _need("kv_len", kv_len, i32, (c.batch,), dev), indptr, indices, group_size, sm_scale,
+        _need("out", out, bf, shape, dev),
+        None if lse is None else _need("lse", lse, torch.float32, shape[:2], dev),
+        None if ws is None else ws.data_ptr(), _nbytes(ws), _stream(stream)))
+    return out, lse

@@ -12,6 +12,7 @@
 #include "compactattn.h"
 #include "common.hpp"
 #include "kernels.hpp"
+#include "serving.hpp"
 
 namespace {
 
@@ -403,6 +404,37 @@ ca_status run_attention(const ca_problem* p, const uint16_t* q, const uint16_t* 
 #endif
   return hip_status(ca::launch_attention(d, L, static_cast<hipStream_t>(stream)),
                     dense ? "dense paged attention launch" : "chunk attention launch");
+}
+
+// Validates c (and group_size when > 0) and fills d.
+ca_status check_cache(const ca_cache* c, int32_t group_size, ca::CacheDims* d) {
+  if (c == nullptr) return fail(CA_ERR_NULL, "cache is NULL");
+  if (c->batch < 1 || c->num_q_heads < 1 || c->num_kv_heads < 1)
+    return fail(CA_ERR_SHAPE, "batch, num_q_heads and num_kv_heads must be >= 1");
+  if (c->num_q_heads % c->num_kv_heads != 0)
+    return fail(CA_ERR_SHAPE, "num_kv_heads (%d) must divide num_q_heads (%d)",
+                c->num_kv_heads, c->num_q_heads);
+  if ((long long)c->batch * c->num_q_heads > INT32_MAX)
+    return fail(CA_ERR_SHAPE, "batch * num_q_heads = %lld does not fit in 31 bits",
+                (long long)c->batch * c->num_q_heads);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(CA_ERR_UNSUPPORTED, "head_dim %d not supported (64, 128)", c->head_dim);
+  if (c->page_size != ca::kPage)
+    return fail(CA_ERR_UNSUPPORTED, "page_size %d not supported (64)", c->page_size);
+  if (c->v_layout != CA_V_TOKEN_MAJOR && c->v_layout != CA_V_TRANSPOSED)
+    return fail(CA_ERR_SHAPE, "v_layout %d is not CA_V_TOKEN_MAJOR (0) or CA_V_TRANSPOSED (1)",
+                c->v_layout);
+  if (c->max_kv_blocks < 1 || c->max_kv_blocks > ca::kMaxKvBlocks)
+    return fail(CA_ERR_SHAPE, "max_kv_blocks %d out of range [1, %d]", c->max_kv_blocks,
+                ca::kMaxKvBlocks);
+  if (c->num_pages < 1) return fail(CA_ERR_SHAPE, "num_pages must be >= 1");
+  if (group_size > 0 && (c->num_q_heads / c->num_kv_heads) % group_size != 0)
+    return fail(CA_ERR_GROUP, "group_size %d must divide Hq/Hkv = %d", group_size,
+                c->num_q_heads / c->num_kv_heads);
+  if (d != nullptr)
+    *d = {c->batch, c->num_q_heads, c->num_kv_heads, c->head_dim, c->max_kv_blocks, c->num_pages,
+          c->v_layout};
+  return ok();
 }
 
 }  // namespace
@@ -902,6 +934,157 @@ ca_status ca_validate_tables(const ca_problem* p, int32_t group_size, const int3
     return s;
   return check_tables(p, d, group_size, ip.data(), ix.data(), nullptr, 0,
                       require_chunk_open != 0);
+}
+
+ca_status ca_check_cache(const ca_cache* c, int32_t group_size) {
+  return check_cache(c, group_size, nullptr);
+}
+
+ca_status ca_assign_slots(const ca_cache* c, const int32_t* new_len, int32_t num_tokens,
+                          const int32_t* seq_len, int32_t* page_table,
+                          const int32_t* free_pages, int32_t free_capacity,
+                          const int32_t* free_count, int64_t* slot_map, int32_t* positions,
+                          int32_t* token_indptr, int32_t* granted, int32_t* seq_len_out,
+                          int32_t* free_count_out, void* stream) {
+  ca::CacheDims d;
+  ca_status s = check_cache(c, 0, &d);
+  if (s != CA_OK) return s;
+  if (num_tokens < 0) return fail(CA_ERR_SHAPE, "num_tokens must be >= 0");
+  if (free_capacity < 0) return fail(CA_ERR_SHAPE, "free_capacity must be >= 0");
+  if (!new_len || !seq_len || !page_table || !free_count || !token_indptr || !granted ||
+      !seq_len_out || !free_count_out)
+    return fail(CA_ERR_NULL,
+                "new_len, seq_len, page_table, free_count, token_indptr, granted, seq_len_out and "
+                "free_count_out are required");
+  if (num_tokens > 0 && (!slot_map || !positions))
+    return fail(CA_ERR_NULL, "slot_map and positions are required");
+  if (free_capacity > 0 && !free_pages) return fail(CA_ERR_NULL, "free_pages is required");
+  if (reinterpret_cast<uintptr_t>(slot_map) % sizeof(int64_t) != 0)
+    return fail(CA_ERR_UNALIGNED, "slot_map must be 8-byte aligned");
+  const ca::SlotLaunch l = {new_len, seq_len, page_table, const_cast<int32_t*>(free_pages),
+                            free_count, slot_map, positions, token_indptr, granted, seq_len_out,
+                            free_count_out, free_capacity, num_tokens};
+  return hip_status(ca::launch_assign_slots(d, l, static_cast<hipStream_t>(stream)),
+                    "assign slots launch");
+}
+
+ca_status ca_release_pages(const ca_cache* c, const int32_t* release, const int32_t* seq_len,
+                           const int32_t* page_table, int32_t* free_pages,
+                           int32_t free_capacity, const int32_t* free_count,
+                           int32_t* seq_len_out, int32_t* free_count_out, void* stream) {
+  ca::CacheDims d;
+  ca_status s = check_cache(c, 0, &d);
+  if (s != CA_OK) return s;
+  if (free_capacity < 0) return fail(CA_ERR_SHAPE, "free_capacity must be >= 0");
+  if (!release || !seq_len || !page_table || !free_count || !seq_len_out || !free_count_out)
+    return fail(CA_ERR_NULL,
+                "release, seq_len, page_table, free_count, seq_len_out and free_count_out are "
+                "required");
+  if (free_capacity > 0 && !free_pages) return fail(CA_ERR_NULL, "free_pages is required");
+  const ca::SlotLaunch l = {release, seq_len, const_cast<int32_t*>(page_table), free_pages,
+                            free_count, nullptr, nullptr, nullptr, nullptr, seq_len_out,
+                            free_count_out, free_capacity, 0};
+  return hip_status(ca::launch_release_pages(d, l, static_cast<hipStream_t>(stream)),
+                    "release pages launch");
+}
+
+ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_tokens,
+                           const uint16_t* q, int64_t q_stride, const uint16_t* k,
+                           int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                           const int32_t* positions, const int64_t* slot_map, uint16_t* q_out,
+                           uint16_t* k_pool, uint16_t* v_pool, void* stream) {
+  ca::CacheDims d;
+  ca_status s = check_cache(c, 0, &d);
+  if (s != CA_OK) return s;
+  if (r == nullptr) return fail(CA_ERR_NULL, "rotary is NULL");
+  if (r->rot_dim < 0 || r->rot_dim > d.D || r->rot_dim % 16 != 0)
+    return fail(CA_ERR_UNSUPPORTED, "rot_dim %d is not a multiple of 16 in [0, %d]", r->rot_dim,
+                d.D);
+  if (r->num_axes < 1 || r->num_axes > 4)
+    return fail(CA_ERR_UNSUPPORTED, "num_axes %d not supported (1 to 4)", r->num_axes);
+  if (r->rot_dim > 0 && !r->inv_freq) return fail(CA_ERR_NULL, "inv_freq is required");
+  if (num_tokens < 0) return fail(CA_ERR_SHAPE, "num_tokens must be >= 0");
+  ca::AppendLaunch l = {};
+  for (int i = 0; r->pair_axis_host && i < r->rot_dim / 2; ++i) {
+    const int axis = r->pair_axis_host[i];
+    if (axis < 0 || axis >= r->num_axes)
+      return fail(CA_ERR_SHAPE, "pair_axis_host[%d] = %d is not in [0, %d)", i, axis, r->num_axes);
+    l.pair_axis[i / 32] |= (uint64_t)axis << (2 * (i % 32));
+  }
+  const int64_t wq = (int64_t)d.Hq * d.D, wk = (int64_t)d.Hkv * d.D;
+  if (num_tokens > 1 && (q_stride < wq || k_stride < wk || v_stride < wk))
+    return fail(CA_ERR_SHAPE, "a token's stride is shorter than its heads");
+  if (q_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0)
+    return fail(CA_ERR_UNALIGNED, "token strides must be multiples of 8 elements");
+  if (num_tokens == 0) return ok();
+  if (!q || !k || !v || !positions || !slot_map || !q_out || !k_pool || !v_pool)
+    return fail(CA_ERR_NULL,
+                "q, k, v, positions, slot_map, q_out, k_pool and v_pool are required");
+  if ((s = need_aligned16("q, k, v, q_out, k_pool and v_pool", q, k, v, q_out, k_pool, v_pool)) !=
+      CA_OK)
+    return s;
+  if (reinterpret_cast<uintptr_t>(slot_map) % sizeof(int64_t) != 0)
+    return fail(CA_ERR_UNALIGNED, "slot_map must be 8-byte aligned");
+  // every work item reads the elements it writes, and only those: q_out may be
+  // q itself, token for token
+  if (q_out == q && q_stride != wq && num_tokens > 1)
+    return fail(CA_ERR_SHAPE, "q_out may be q only if q is dense");
+  l.q = q;
+  l.k = k;
+  l.v = v;
+  l.q_stride = q_stride;
+  l.k_stride = k_stride;
+  l.v_stride = v_stride;
+  l.positions = positions;
+  l.slot_map = slot_map;
+  l.inv_freq = r->inv_freq;
+  l.q_out = q_out;
+  l.k_pool = k_pool;
+  l.v_pool = v_pool;
+  l.num_tokens = num_tokens;
+  l.rot_dim = r->rot_dim;
+  l.num_axes = r->num_axes;
+  l.interleaved = r->interleaved != 0;
+  return hip_status(ca::launch_rotary_append(d, l, static_cast<hipStream_t>(stream)),
+                    "rotary append launch");
+}
+
+size_t ca_decode_workspace_bytes(const ca_cache* c, int32_t group_size) {
+  ca::CacheDims d;
+  if (group_size < 0 || check_cache(c, group_size, &d) != CA_OK) return 0;
+  return ca::decode_ws_bytes(d, group_size > 0 ? group_size : d.Hq / d.Hkv);
+}
+
+ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16_t* k_pool,
+                              const uint16_t* v_pool, const int32_t* page_table,
+                              const int32_t* kv_len, const int32_t* kv_indptr,
+                              const int32_t* kv_indices, int32_t group_size, float sm_scale,
+                              uint16_t* out, float* lse, void* ws, size_t ws_bytes,
+                              void* stream) {
+  ca::CacheDims d;
+  if (group_size < 0) return fail(CA_ERR_GROUP, "group_size must be >= 0");
+  ca_status s = check_cache(c, group_size, &d);
+  if (s != CA_OK) return s;
+  if (!q || !k_pool || !v_pool || !page_table || !kv_len || !out)
+    return fail(CA_ERR_NULL, "q, k_pool, v_pool, page_table, kv_len and out are required");
+  if ((kv_indptr == nullptr) != (kv_indices == nullptr))
+    return fail(CA_ERR_NULL, "kv_indptr and kv_indices come together");
+  if ((s = need_aligned16("q, k_pool, v_pool and out", q, k_pool, v_pool, out)) != CA_OK) return s;
+  if (!(sm_scale > 0.f) || !std::isfinite(sm_scale))
+    return fail(CA_ERR_SHAPE, "sm_scale must be finite and > 0, got %g", (double)sm_scale);
+  const int ratio = d.Hq / d.Hkv;
+  // without tables every head of a KV head reads the same blocks
+  const int gs = kv_indptr && group_size > 0 ? group_size : ratio;
+  const size_t need = ca::decode_ws_bytes(d, gs);
+  if (need > 0 && (ws == nullptr || ws_bytes < need))
+    return fail(CA_ERR_WORKSPACE, "decode attention needs %zu workspace bytes, got %zu", need,
+                ws == nullptr ? (size_t)0 : ws_bytes);
+  if (reinterpret_cast<uintptr_t>(ws) % 16 != 0)
+    return fail(CA_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+  const ca::DecodeLaunch l = {q, k_pool, v_pool, page_table, kv_len, kv_indptr, kv_indices, out,
+                              lse, ws, gs, sm_scale};
+  return hip_status(ca::launch_decode(d, l, static_cast<hipStream_t>(stream)),
+                    "decode attention launch");
 }
 
 }  // extern "C"
