@@ -405,7 +405,7 @@ ca_status ca_packed_chunk_attention(const ca_problem* p, const uint16_t* q,
  * ---------------------------------------------------------------------- */
 typedef struct ca_cache {
   int32_t batch;             /* B >= 1: requests, the rows of page_table        */
-  int32_t num_q_heads;       /* Hq, B * Hq < 2^31                               */
+  int32_t num_q_heads;       /* Hq <= 65536, B * Hq < 2^31                      */
   int32_t num_kv_heads;      /* Hkv, divides Hq                                 */
   int32_t head_dim;          /* D, 64 or 128                                    */
   int32_t page_size;         /* tokens per page; must be 64                     */

@@ -414,9 +414,9 @@ ca_status check_cache(const ca_cache* c, int32_t group_size, ca::CacheDims* d) {
   if (c->num_q_heads % c->num_kv_heads != 0)
     return fail(CA_ERR_SHAPE, "num_kv_heads (%d) must divide num_q_heads (%d)",
                 c->num_kv_heads, c->num_q_heads);
-  if ((long long)c->batch * c->num_q_heads > INT32_MAX)
-    return fail(CA_ERR_SHAPE, "batch * num_q_heads = %lld does not fit in 31 bits",
-                (long long)c->batch * c->num_q_heads);
+  if (c->num_q_heads > 65536 || (long long)c->batch * c->num_q_heads > INT32_MAX)
+    return fail(CA_ERR_SHAPE, "num_q_heads %d > 65536, or batch * num_q_heads >= 2^31",
+                c->num_q_heads);
   if (c->head_dim != 64 && c->head_dim != 128)
     return fail(CA_ERR_UNSUPPORTED, "head_dim %d not supported (64, 128)", c->head_dim);
   if (c->page_size != ca::kPage)

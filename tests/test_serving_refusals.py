@@ -30,7 +30,7 @@ def _name(lib, status):
     (dict(batch=0), 0, "CA_ERR_SHAPE"), (dict(num_kv_heads=3), 0, "CA_ERR_SHAPE"),
     (dict(max_kv_blocks=0), 0, "CA_ERR_SHAPE"), (dict(max_kv_blocks=16385), 0, "CA_ERR_SHAPE"),
     (dict(num_pages=0), 0, "CA_ERR_SHAPE"), (dict(v_layout=2), 0, "CA_ERR_SHAPE"),
-    (dict(batch=1 << 30), 0, "CA_ERR_SHAPE"), (dict(), 3, "CA_ERR_GROUP"), (dict(), 8, "CA_ERR_GROUP"),
+    (dict(batch=1 << 30), 0, "CA_ERR_SHAPE"), (dict(num_q_heads=1 << 17), 0, "CA_ERR_SHAPE"), (dict(), 3, "CA_ERR_GROUP"), (dict(), 8, "CA_ERR_GROUP"),
 ])
 def test_check_cache(lib, kw, group, code):
     assert _name(lib, lib.ca_check_cache(_cache(**kw).ref, group)) == code
@@ -125,6 +125,7 @@ def _decode(lib, q=FAKE, kp=FAKE, vp=FAKE, pt=FAKE, kl=FAKE, ip=None, ix=None, g
     (dict(scale=float("nan")), "CA_ERR_SHAPE"), (dict(scale=float("inf")), "CA_ERR_SHAPE"),
     (dict(q=FAKE + 8), "CA_ERR_UNALIGNED"), (dict(out=FAKE + 2), "CA_ERR_UNALIGNED"),
     (dict(kp=FAKE + 8), "CA_ERR_UNALIGNED"), (dict(ws=FAKE + 8), "CA_ERR_WORKSPACE"),
+    (dict(ws=None), "CA_ERR_WORKSPACE"), (dict(nbytes=1000), "CA_ERR_WORKSPACE"),
 ] + [({n: None}, "CA_ERR_NULL") for n in ("q", "kp", "vp", "pt", "kl", "out")])
 def test_decode_attention_refuses(lib, kw, code):
     assert _decode(lib, **kw) == code
