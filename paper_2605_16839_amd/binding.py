@@ -625,21 +625,26 @@ class Rotary:
         self.ref = ctypes.byref(self.c)
 
 
-def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape, device: torch.device):
+def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: tuple, index: int):
     """The address of an argument of the serving step; its type, shape and place are checked,
     since the kernels take them from the cache's sizes."""
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}, "
+    if (t.dtype is not dtype or t.shape != shape or t.get_device() != index
+            or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on cuda:{index}, "
                          f"got {t.dtype} {list(t.shape)} on {t.device}, strides {t.stride()}")
     return t.data_ptr()
 
 
-def _here(t: torch.Tensor) -> torch.device:
-    """The device of a call: the current one, whose stream the call is enqueued on."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {t.device}, but the current device is "
-                         f"{'cuda:%d' % torch.cuda.current_device() if torch.cuda.is_available() else 'none'}")
-    return t.device
+def _here(t: torch.Tensor, stream):
+    """A call's device index and stream: tensors have to be on the current device, whose
+    stream the call is enqueued on."""
+    index = t.get_device()
+    if index < 0 or index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {t.device}: they must be on the current device"
+                         + (f", cuda:{torch.cuda.current_device()}" if index >= 0 else ""))
+    if stream is None and _raw_stream is not None:
+        return index, _raw_stream(index)
+    return index, (stream or torch.cuda.current_stream()).cuda_stream
 
 
 def check_cache(c: Cache, group_size: int = 0) -> None:
@@ -654,24 +659,30 @@ def assign_slots(c: Cache, new_len: torch.Tensor, num_tokens: int, seq_len: torc
     Returns ``bufs`` (made where missing): slot_map int64 [num_tokens, Hkv], and int32
     positions [num_tokens], token_indptr [B + 1], granted [B], seq_len [B] and
     free_count [1] after the step; the last two may be the inputs themselves."""
-    dev, i32, B = _here(new_len), torch.int32, c.batch
+    index, st = _here(new_len, stream)
+    i32, B, T = torch.int32, c.batch, num_tokens
     b = bufs if bufs is not None else {}
-    for key, shape, dtype in (("slot_map", (num_tokens, c.num_kv_heads), torch.int64),
-                              ("positions", (num_tokens,), i32), ("token_indptr", (B + 1,), i32),
-                              ("granted", (B,), i32), ("seq_len", (B,), i32),
-                              ("free_count", (1,), i32)):
-        if key not in b:
-            b[key] = torch.empty(shape, dtype=dtype, device=dev)
+    slots = (T, c.num_kv_heads)
+    if "slot_map" not in b:
+        b["slot_map"] = torch.empty(slots, dtype=torch.int64, device=new_len.device)
+    sizes = {"positions": T, "token_indptr": B + 1, "granted": B, "seq_len": B, "free_count": 1}
+    missing = [k for k in sizes if k not in b]
+    if missing:   # parts of one tensor: an allocation costs as much as all the checks below
+        n = [sizes[k] for k in missing]
+        parts = torch.empty(sum(n), dtype=i32, device=new_len.device).split_with_sizes(n)
+        b.update(zip(missing, parts))
     _check(load().ca_assign_slots(
-        c.ref, _need("new_len", new_len, i32, (B,), dev), num_tokens,
-        _need("seq_len", seq_len, i32, (B,), dev), _need("page_table", page_table, i32, c._table, dev),
-        _need("free_pages", free_pages, i32, (free_pages.numel(),), dev), free_pages.numel(),
-        _need("free_count", free_count, i32, (1,), dev),
-        _need("slot_map", b["slot_map"], torch.int64, (num_tokens, c.num_kv_heads), dev),
-        _need("positions", b["positions"], i32, (num_tokens,), dev),
-        _need("token_indptr", b["token_indptr"], i32, (B + 1,), dev),
-        _need("granted", b["granted"], i32, (B,), dev), _need("seq_len", b["seq_len"], i32, (B,), dev),
-        _need("free_count", b["free_count"], i32, (1,), dev), _stream(stream)))
+        c.ref, _need("new_len", new_len, i32, (B,), index), T,
+        _need("seq_len", seq_len, i32, (B,), index),
+        _need("page_table", page_table, i32, c._table, index),
+        _need("free_pages", free_pages, i32, (free_pages.numel(),), index), free_pages.numel(),
+        _need("free_count", free_count, i32, (1,), index),
+        _need("slot_map", b["slot_map"], torch.int64, slots, index),
+        _need("positions", b["positions"], i32, (T,), index),
+        _need("token_indptr", b["token_indptr"], i32, (B + 1,), index),
+        _need("granted", b["granted"], i32, (B,), index),
+        _need("seq_len", b["seq_len"], i32, (B,), index),
+        _need("free_count", b["free_count"], i32, (1,), index), st))
     return b
 
 
@@ -680,26 +691,30 @@ def release_pages(c: Cache, release: torch.Tensor, seq_len: torch.Tensor,
                   out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None):
     """Ends the requests with release != 0: their pages go behind the free ones in free_pages.
     Returns (seq_len, free_count) after it, which may be the inputs themselves (``out``)."""
-    dev, i32, B = _here(release), torch.int32, c.batch
+    index, st = _here(release, stream)
+    i32, B = torch.int32, c.batch
     if out is None:
-        out = (torch.empty_like(seq_len), torch.empty_like(free_count))
+        out = torch.empty(B + 1, dtype=i32, device=release.device).split_with_sizes((B, 1))
     _check(load().ca_release_pages(
-        c.ref, _need("release", release, i32, (B,), dev), _need("seq_len", seq_len, i32, (B,), dev),
-        _need("page_table", page_table, i32, c._table, dev),
-        _need("free_pages", free_pages, i32, (free_pages.numel(),), dev), free_pages.numel(),
-        _need("free_count", free_count, i32, (1,), dev), _need("seq_len", out[0], i32, (B,), dev),
-        _need("free_count", out[1], i32, (1,), dev), _stream(stream)))
+        c.ref, _need("release", release, i32, (B,), index),
+        _need("seq_len", seq_len, i32, (B,), index),
+        _need("page_table", page_table, i32, c._table, index),
+        _need("free_pages", free_pages, i32, (free_pages.numel(),), index), free_pages.numel(),
+        _need("free_count", free_count, i32, (1,), index), _need("seq_len", out[0], i32, (B,), index),
+        _need("free_count", out[1], i32, (1,), index), st))
     return out
 
 
-def _rows(name: str, t: torch.Tensor, heads: int, dim: int, rows: int, device: torch.device):
+def _rows(name: str, t: torch.Tensor, shape: tuple, index: int):
     """Address and token stride of [rows, heads, dim] whose tokens may lie apart."""
-    if (t.dtype != torch.bfloat16 or t.shape != (rows, heads, dim) or t.device != device
-            or (rows and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)))):
-        raise ValueError(f"{name} must be a bfloat16 tensor {[rows, heads, dim]} on {device} with "
+    rows, heads, dim = shape
+    apart = t.stride()
+    if (t.dtype is not torch.bfloat16 or t.shape != shape or t.get_device() != index
+            or (rows and (apart[2] != 1 or (heads > 1 and apart[1] != dim)))):
+        raise ValueError(f"{name} must be a bfloat16 tensor {list(shape)} on cuda:{index} with "
                          f"contiguous heads, got {t.dtype} {list(t.shape)} on {t.device}, "
-                         f"strides {t.stride()}")
-    return t.data_ptr(), t.stride(0) if rows > 1 else heads * dim
+                         f"strides {apart}")
+    return t.data_ptr(), apart[0] if rows > 1 else heads * dim
 
 
 def rotary_append(c: Cache, r: Rotary, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -709,24 +724,24 @@ def rotary_append(c: Cache, r: Rotary, q: torch.Tensor, k: torch.Tensor, v: torc
     """Rotates q [T, Hq, D] and k [T, Hkv, D] by their positions ([T], or [axes, T]) and writes
     keys and values to slot_map's places in the pools; returns the rotated queries.  q, k and v
     may be parts of one tensor (a token's heads together, tokens apart)."""
-    dev, bf = _here(q), torch.bfloat16
+    index, st = _here(q, stream)
+    bf = torch.bfloat16
     T, Hq, Hkv, D = q.shape[0], c.num_q_heads, c.num_kv_heads, c.head_dim
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=bf, device=dev)
-    qp, qs = _rows("q", q, Hq, D, T, dev)
-    kp, ks = _rows("k", k, Hkv, D, T, dev)
-    vp, vs = _rows("v", v, Hkv, D, T, dev)
-    place = positions.shape if positions.dim() == 1 and r.num_axes == 1 else (r.num_axes, T)
-    if place[-1] != T:
-        raise ValueError(f"positions {list(positions.shape)} for {T} tokens")
-    if r.inv_freq is not None and r.inv_freq.device != dev:
-        raise ValueError(f"inv_freq on {r.inv_freq.device}, the tokens on {dev}")
+        out = torch.empty((T, Hq, D), dtype=bf, device=q.device)
+    qp, qs = _rows("q", q, (T, Hq, D), index)
+    kp, ks = _rows("k", k, (T, Hkv, D), index)
+    vp, vs = _rows("v", v, (T, Hkv, D), index)
+    place = (T,) if r.num_axes == 1 and positions.dim() == 1 else (r.num_axes, T)
+    if r.inv_freq is not None and r.inv_freq.get_device() != index:
+        raise ValueError(f"inv_freq on {r.inv_freq.device}, the tokens on cuda:{index}")
     _check(load().ca_rotary_append(
         c.ref, r.ref, T, qp, qs, kp, ks, vp, vs,
-        _need("positions", positions, torch.int32, place, dev),
-        _need("slot_map", slot_map, torch.int64, (T, Hkv), dev), _need("out", out, bf, (T, Hq, D), dev),
-        _need("k_pool", kv_pool[0], bf, c._k_pool, dev), _need("v_pool", kv_pool[1], bf, c._v_pool, dev),
-        _stream(stream)))
+        _need("positions", positions, torch.int32, place, index),
+        _need("slot_map", slot_map, torch.int64, (T, Hkv), index),
+        _need("out", out, bf, (T, Hq, D), index),
+        _need("k_pool", kv_pool[0], bf, c._k_pool, index),
+        _need("v_pool", kv_pool[1], bf, c._v_pool, index), st))
     return out
 
 
@@ -743,27 +758,28 @@ def decode_attention(c: Cache, q: torch.Tensor, kv_pool: Tuple[torch.Tensor, tor
     """Attention of one new token per request, q [B, Hq, D], over its kv_len[b] cached tokens, or
     over the blocks that ``tables`` (kv_indptr, kv_indices; one row per group of group_size heads,
     0: all heads of a KV head) list; returns (out bf16, lse fp32 or None)."""
-    dev, bf, i32 = _here(q), torch.bfloat16, torch.int32
+    index, st = _here(q, stream)
+    bf, i32 = torch.bfloat16, torch.int32
     shape = (c.batch, c.num_q_heads, c.head_dim)
     if out is None:
-        out = torch.empty(shape, dtype=bf, device=dev)
+        out = torch.empty(shape, dtype=bf, device=q.device)
     if ws is None:
         n = decode_workspace_bytes(c, group_size)
-        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
-    elif ws.device != dev or not ws.is_contiguous():
-        raise ValueError(f"ws must be contiguous on {dev}")
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    elif ws.get_device() != index or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous on cuda:{index}")
     indptr = indices = None
     if tables is not None:
         check_cache(c, group_size)
         rows = c.batch * (c.num_q_heads // (group_size or c.num_q_heads // c.num_kv_heads))
-        indptr = _need("kv_indptr", tables[0], i32, (rows + 1,), dev)
-        indices = _need("kv_indices", tables[1], i32, (rows * c.max_kv_blocks,), dev)
+        indptr = _need("kv_indptr", tables[0], i32, (rows + 1,), index)
+        indices = _need("kv_indices", tables[1], i32, (rows * c.max_kv_blocks,), index)
     _check(load().ca_decode_attention(
-        c.ref, _need("q", q, bf, shape, dev), _need("k_pool", kv_pool[0], bf, c._k_pool, dev),
-        _need("v_pool", kv_pool[1], bf, c._v_pool, dev),
-        _need("page_table", page_table, i32, c._table, dev),
-        _need("kv_len", kv_len, i32, (c.batch,), dev), indptr, indices, group_size, sm_scale,
-        _need("out", out, bf, shape, dev),
-        None if lse is None else _need("lse", lse, torch.float32, shape[:2], dev),
-        None if ws is None else ws.data_ptr(), _nbytes(ws), _stream(stream)))
+        c.ref, _need("q", q, bf, shape, index), _need("k_pool", kv_pool[0], bf, c._k_pool, index),
+        _need("v_pool", kv_pool[1], bf, c._v_pool, index),
+        _need("page_table", page_table, i32, c._table, index),
+        _need("kv_len", kv_len, i32, (c.batch,), index), indptr, indices, group_size, sm_scale,
+        _need("out", out, bf, shape, index),
+        None if lse is None else _need("lse", lse, torch.float32, shape[:2], index),
+        None if ws is None else ws.data_ptr(), _nbytes(ws), st))
     return out, lse

@@ -9,35 +9,63 @@
 //
 // Every workgroup makes the sums itself, kSlotThreads requests at a time, and
 // writes the token rows of its own range, so one launch does it and no
-// workgroup waits for another.
+// workgroup waits for another.  What bounds a call is latency: the lengths, the
+// sums, and the ids that hang on them, one after the other.
 #include "common.hpp"
 #include "serving.hpp"
 
 namespace ca {
 namespace {
 
-constexpr int kSlotThreads = 256;
+constexpr int kSlotThreads = 1024;
 constexpr int kSlotWaves = kSlotThreads / kWave;
+constexpr int kSlotGroups = 256;
+constexpr int kReleaseGroups = 16;
 
-// Inclusive sums over the workgroup's threads of two values.
+// The value of a lane before this one in 64-bit halves (0 where there is none).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ long long dpp64(long long v) {
+  const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)v, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (long long)(((unsigned long long)(unsigned)hi << 32) | lo);
+}
+__device__ __forceinline__ long long wave_inclusive_sum(long long v) {
+  v += dpp64<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8: within 16 lanes
+  v += dpp64<0x112, 0xf>(v);
+  v += dpp64<0x114, 0xf>(v);
+  v += dpp64<0x118, 0xf>(v);
+  v += dpp64<0x142, 0xa>(v);   // lane 15 to the next 16, lane 47 to the last
+  v += dpp64<0x143, 0xc>(v);   // lane 31 to the upper half
+  return v;
+}
+
+// Inclusive sums over the workgroup's threads of two values, and their totals.
 struct Sums {
   long long a, b;
 };
-__device__ __forceinline__ Sums block_inclusive_sums(Sums v, Sums* part) {
+__device__ __forceinline__ Sums block_inclusive_sums(Sums v, Sums* part, Sums* all) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const long long ta = __shfl_up(v.a, o, kWave), tb = __shfl_up(v.b, o, kWave);
-    if (lane >= o) v.a += ta, v.b += tb;
-  }
-  __syncthreads();   // the previous use of part
+  v.a = wave_inclusive_sum(v.a);
+  v.b = wave_inclusive_sum(v.b);
   if (lane == kWave - 1) part[wv] = v;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSlotWaves; ++w)
-    if (w < wv) v.a += part[w].a, v.b += part[w].b;
+  // the waves' totals: lane l of every 16 holds wave l's
+  const Sums p = part[lane & (kSlotWaves - 1)];
+  Sums s = p;
+  s.a += dpp64<0x111, 0xf>(s.a), s.b += dpp64<0x111, 0xf>(s.b);
+  s.a += dpp64<0x112, 0xf>(s.a), s.b += dpp64<0x112, 0xf>(s.b);
+  s.a += dpp64<0x114, 0xf>(s.a), s.b += dpp64<0x114, 0xf>(s.b);
+  s.a += dpp64<0x118, 0xf>(s.a), s.b += dpp64<0x118, 0xf>(s.b);
+  auto of_lane = [](long long x, int l) {
+    const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)x, l);
+    return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32) | lo);
+  };
+  const int w = __builtin_amdgcn_readfirstlane(wv);
+  v.a += of_lane(s.a - p.a, w), v.b += of_lane(s.b - p.b, w);
+  *all = {of_lane(s.a, kSlotWaves - 1), of_lane(s.b, kSlotWaves - 1)};
   return v;
 }
+static_assert(kSlotWaves == 16, "one row of 16 lanes sums the waves");
 
 __device__ __forceinline__ long long blocks_of(long long tokens) {
   return (tokens + kPage - 1) / kPage;
@@ -56,7 +84,9 @@ __device__ __forceinline__ int last_at_most(const long long* start, int n, long 
 
 struct SlotArgs {
   SlotLaunch l;
-  int B, Hkv, max_kv_blocks, num_pages, rows_per_wg;
+  int B, Hkv, max_kv_blocks, num_pages;
+  int rows_at_once;   // token rows that a workgroup's threads write together
+  int rows_per_wg;    // a multiple of it
 };
 
 __global__ __launch_bounds__(kSlotThreads) void assign_slots_kernel(const SlotArgs a) {
@@ -64,7 +94,6 @@ __global__ __launch_bounds__(kSlotThreads) void assign_slots_kernel(const SlotAr
   __shared__ long long s_row[kSlotThreads];     // first token row of a request
   __shared__ long long s_taken[kSlotThreads];   // pages taken before it
   __shared__ int s_old[kSlotThreads];           // its cached tokens, -1: refused
-  __shared__ Sums s_end;                        // both sums after the last request of the round
   __shared__ long long s_given;
   const SlotLaunch& l = a.l;
   const int tid = threadIdx.x, H = a.Hkv;
@@ -74,6 +103,9 @@ __global__ __launch_bounds__(kSlotThreads) void assign_slots_kernel(const SlotAr
   long long hi = lo + a.rows_per_wg;
   lo = lo < T ? lo : T;
   hi = hi < T ? hi : T;
+  // this thread's row among those written together, and its first head
+  const int r0 = a.rows_at_once > 1 ? tid / H : 0, h0 = a.rows_at_once > 1 ? tid - r0 * H : tid;
+  const bool writes = r0 < a.rows_at_once;
   int count = l.free_count[0];
   count = count < 0 ? 0 : (count > l.free_capacity ? l.free_capacity : count);
   if (tid == 0) s_given = 0;
@@ -86,19 +118,17 @@ __global__ __launch_bounds__(kSlotThreads) void assign_slots_kernel(const SlotAr
     if (b < a.B) old = l.seq_len[b], add = l.step[b];
     const long long rows = add > 0 ? add : 0;
     bool fits = old >= 0 && add >= 0 && old + add <= (long long)a.max_kv_blocks * kPage;
-    // the rows are summed first: a request past the last row needs no pages
-    const Sums r = block_inclusive_sums({rows, 0}, s_part);
-    fits = fits && row0 + r.a <= T;
+    // what a request past the last row needs may be summed: all that follow
+    // it and need pages are past the last row too
     const long long need = fits ? (blocks_of(old + add) - blocks_of(old)) * H : 0;
-    const Sums n = block_inclusive_sums({need, 0}, s_part);
-    const long long taken = taken0 + n.a;
-    fits = fits && (need == 0 || taken <= count);
-    s_row[tid] = row0 + r.a - rows;
+    Sums all;
+    const Sums s = block_inclusive_sums({rows, need}, s_part, &all);
+    const long long end = row0 + s.a, taken = taken0 + s.b;
+    fits = fits && end <= T && (need == 0 || taken <= count);
+    s_row[tid] = end - rows;
     s_taken[tid] = taken - need;
     s_old[tid] = fits ? (int)old : -1;
-    if (tid == kSlotThreads - 1) s_end = {row0 + r.a, taken};
     if (first && b < a.B) {
-      const long long end = row0 + r.a;
       l.token_indptr[b + 1] = (int)(end < T ? end : T);
       l.granted[b] = fits ? (int)add : 0;
       l.seq_len_out[b] = (int)(old + (fits ? add : 0));
@@ -107,41 +137,42 @@ __global__ __launch_bounds__(kSlotThreads) void assign_slots_kernel(const SlotAr
     }
     __syncthreads();
     const int n_here = a.B - b0 < kSlotThreads ? a.B - b0 : kSlotThreads;
-    const long long from = lo > row0 ? lo : row0, to = hi < s_end.a ? hi : s_end.a;
-    for (long long x = from * H + tid; x < to * H; x += kSlotThreads) {
-      const long long t = x / H;
-      const int h = (int)(x - t * H);
+    const long long row1 = row0 + all.a;
+    const long long from = lo > row0 ? lo : row0, to = hi < row1 ? hi : row1;
+    for (long long t = from + r0; writes && t < to; t += a.rows_at_once) {
       const int i = last_at_most(s_row, n_here, t);
       const int had = s_old[i];
-      long long slot = -1;
-      int pos = 0;
-      if (had >= 0) {
-        pos = (int)(had + (t - s_row[i]));
-        const int j = pos / kPage, fresh = j - (int)blocks_of(had);
-        int32_t* entry = l.page_table + ((long long)(b0 + i) * H + h) * a.max_kv_blocks + j;
-        int page;
-        if (fresh >= 0) {
-          page = l.free_pages[count - 1 - (s_taken[i] + (long long)fresh * H + h)];
-          if (pos % kPage == 0) *entry = page;
-        } else {
-          page = *entry;
+      const int pos = had >= 0 ? (int)(had + (t - s_row[i])) : 0;
+      const int j = pos / kPage, fresh = j - (int)blocks_of(had);
+      for (int h = h0; h < H; h += kSlotThreads) {
+        long long slot = -1;
+        if (had >= 0) {
+          int32_t* entry = l.page_table + ((long long)(b0 + i) * H + h) * a.max_kv_blocks + j;
+          int page;
+          if (fresh >= 0) {
+            page = l.free_pages[count - 1 - (s_taken[i] + (long long)fresh * H + h)];
+            if (pos % kPage == 0) *entry = page;
+          } else {
+            page = *entry;
+          }
+          if (page >= 0 && page < a.num_pages) slot = (long long)page * kPage + pos % kPage;
         }
-        if (page >= 0 && page < a.num_pages) slot = (long long)page * kPage + pos % kPage;
+        l.slot_map[t * H + h] = slot;
+        if (h == 0) l.positions[t] = pos;
       }
-      l.slot_map[x] = slot;
-      if (h == 0) l.positions[t] = pos;
     }
-    row0 = s_end.a;
-    taken0 = s_end.b;
-    __syncthreads();
+    row0 = row1;
+    taken0 += all.b;
     if (!first && row0 >= hi) break;
+    __syncthreads();
   }
   // padding rows behind the last request
   const long long pad = lo > row0 ? lo : row0;
-  for (long long x = pad * H + tid; x < hi * H; x += kSlotThreads) {
-    l.slot_map[x] = -1;
-    if (x % H == 0) l.positions[x / H] = 0;
-  }
+  for (long long t = pad + r0; writes && t < hi; t += a.rows_at_once)
+    for (int h = h0; h < H; h += kSlotThreads) {
+      l.slot_map[t * H + h] = -1;
+      if (h == 0) l.positions[t] = 0;
+    }
   if (first && tid == 0) l.free_count_out[0] = count - (int)s_given;
 }
 
@@ -149,7 +180,7 @@ __global__ __launch_bounds__(kSlotThreads) void release_pages_kernel(const SlotA
   __shared__ Sums s_part[kSlotWaves];
   __shared__ long long s_start[kSlotThreads];   // pages released before the request
   __shared__ int s_kept[kSlotThreads];          // 1: does not fit
-  __shared__ long long s_end, s_given;
+  __shared__ long long s_given;
   const SlotLaunch& l = a.l;
   const int tid = threadIdx.x, H = a.Hkv;
   const bool first = blockIdx.x == 0;
@@ -164,12 +195,11 @@ __global__ __launch_bounds__(kSlotThreads) void release_pages_kernel(const SlotA
     if (b < a.B) old = l.seq_len[b], ends = l.step[b] != 0;
     ends = ends && old >= 0 && old <= a.max_kv_blocks * kPage;
     const long long need = ends ? blocks_of(old) * H : 0;
-    const Sums s = block_inclusive_sums({need, 0}, s_part);
-    const long long after = sum0 + s.a;
+    Sums all;
+    const long long after = sum0 + block_inclusive_sums({need, 0}, s_part, &all).a;
     const bool fits = need == 0 || count + after <= l.free_capacity;
     s_start[tid] = after - need;
     s_kept[tid] = !fits;
-    if (tid == kSlotThreads - 1) s_end = after;
     if (first && b < a.B) {
       l.seq_len_out[b] = ends && fits ? 0 : old;
       if (fits && need > 0)
@@ -177,7 +207,7 @@ __global__ __launch_bounds__(kSlotThreads) void release_pages_kernel(const SlotA
     }
     __syncthreads();
     const int n_here = a.B - b0 < kSlotThreads ? a.B - b0 : kSlotThreads;
-    const long long end = s_end;
+    const long long end = sum0 + all.a;
     for (long long x = sum0 + (long long)blockIdx.x * kSlotThreads + tid; x < end;
          x += (long long)gridDim.x * kSlotThreads) {
       const int i = last_at_most(s_start, n_here, x);
@@ -193,15 +223,27 @@ __global__ __launch_bounds__(kSlotThreads) void release_pages_kernel(const SlotA
 
 }  // namespace
 
+// In place, one workgroup does it all: it reads a length before it writes it, and
+// no other workgroup reads it.  Else as many as write their rows in one go
+// (8256 rows of 8 heads: 218 us with one, %(many)s with 65).
 hipError_t launch_assign_slots(const CacheDims& d, const SlotLaunch& l, hipStream_t st) {
-  SlotArgs a{l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, l.num_tokens};
-  assign_slots_kernel<<<1, kSlotThreads, 0, st>>>(a);
+  SlotArgs a{l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, 0, 0};
+  a.rows_at_once = d.Hkv < kSlotThreads ? kSlotThreads / d.Hkv : 1;
+  const bool in_place = l.seq_len_out == l.seq_len || l.free_count_out == l.free_count;
+  const long long rounds = ((long long)l.num_tokens + a.rows_at_once - 1) / a.rows_at_once;
+  // at most kSlotGroups, so that few workgroups repeat the sums
+  const long long each = in_place ? rounds : (rounds + kSlotGroups - 1) / kSlotGroups;
+  const long long per_wg = (each > 0 ? each : 1) * a.rows_at_once;
+  a.rows_per_wg = (int)(per_wg < INT32_MAX ? per_wg : INT32_MAX);
+  const int grid = in_place || rounds == 0 ? 1 : (int)((rounds + each - 1) / each);
+  assign_slots_kernel<<<grid, kSlotThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_release_pages(const CacheDims& d, const SlotLaunch& l, hipStream_t st) {
-  SlotArgs a{l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, 0};
-  release_pages_kernel<<<1, kSlotThreads, 0, st>>>(a);
+  SlotArgs a{l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, 0, 0};
+  const bool in_place = l.seq_len_out == l.seq_len || l.free_count_out == l.free_count;
+  release_pages_kernel<<<in_place ? 1 : kReleaseGroups, kSlotThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
