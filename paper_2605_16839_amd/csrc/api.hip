@@ -1075,6 +1075,9 @@ ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16
   const int ratio = d.Hq / d.Hkv;
   // without tables every head of a KV head reads the same blocks
   const int gs = kv_indptr && group_size > 0 ? group_size : ratio;
+  if ((long long)d.B * (kv_indptr ? d.Hq / gs : 1) * d.max_kv_blocks > INT32_MAX)
+    return fail(CA_ERR_SHAPE, "the rows' blocks (batch x max_kv_blocks, with tables x groups) "
+                "must be fewer than 2^31");
   const size_t need = ca::decode_ws_bytes(d, gs);
   if (need > 0 && (ws == nullptr || ws_bytes < need))
     return fail(CA_ERR_WORKSPACE, "decode attention needs %zu workspace bytes, got %zu", need,

@@ -8,7 +8,7 @@
 //   * the requests' lengths are on the GPU only and may be as different as they
 //     like, so the pages of all (request, KV head) rows are laid end to end and
 //     cut in equal shares, one per workgroup and within it one per wave; every
-//     workgroup finds its share from a prefix sum over the lengths;
+//     wave finds its share from a prefix sum over the lengths;
 //   * a wave is on its own until its share ends: it loads K and V pages to
 //     registers (32 KB of them in flight per wave, 256 KB per CU), and no
 //     barrier or other wave is waited for;
@@ -22,7 +22,12 @@
 //     so the weights count with 16 bits at no cost;
 //   * a row that lies inside one wave's share is written at once; pieces of
 //     a workgroup's waves are joined in its LDS, and rows that several workgroups
-//     share by a second launch (decode_join_kernel).
+//     share by the last of them (join_row).
+#include <atomic>
+#include <chrono>
+#include <cstdint>
+#include <random>
+
 #include "common.hpp"
 #include "serving.hpp"
 
@@ -32,25 +37,21 @@ namespace {
 constexpr int kWaves = 8;                   // per workgroup
 constexpr int kThreads = kWaves * kWave;
 constexpr int kGroups = 256;                // one workgroup per CU
-constexpr int kMinPages = 4;                // of a workgroup's share
+constexpr int kMinPages = 2 * kWaves;       // of a workgroup's share
 constexpr int kTileHeads = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-
-struct Share {   // what decode_join_kernel has to know about a workgroup's share
-  long long row_end;   // end (in pages) of the row that goes on after the share, 0: none
-  long long total;     // pages of all rows
-  int out_row;         // that row's first output head (b * Hq + head)
-  int heads;
-};
 
 struct DecodeArgs {
   DecodeLaunch l;
   int B, Hq, Hkv, G, HT, items, per_item, max_kv_blocks, num_pages;
   float scale_log2;
-  float4* part_o;    // [kGroups][2][D / 16][64]: O^T fragments as the registers lie
-  float2* part_ml;   // [kGroups][2][16]: maximum (log2 units) and sum
-  Share* shares;     // [kGroups]
+  // pieces that a workgroup leaves to others: [0] of the row that its share
+  // starts in the middle of, [1] of the row that goes on after its share
+  float* part_o;                    // [kGroups][2][16][D]
+  float* part_ml;                   // [kGroups][2][16][2]: maximum (log2 units) and sum
+  unsigned long long* arrived;      // [kGroups][2]: tag once a piece is there
+  unsigned long long tag;           // this launch's, never 0
 };
 
 template <typename T>
@@ -91,11 +92,27 @@ __device__ __forceinline__ float other_half(float x) {
 // 2^x, and the maxima in log2 units: exp2 of -inf is 0.
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// First page of share w when `total` pages are dealt.
+// First page of share w when `total` pages are dealt, and the share of page u.
 __device__ __forceinline__ long long share_start(long long total, int w) {
   if (total >= (long long)kGroups * kMinPages) return (total * w) / kGroups;
   const long long s = (long long)w * kMinPages;
   return s < total ? s : total;
+}
+__device__ __forceinline__ int share_of(long long total, long long u) {
+  if (total < (long long)kGroups * kMinPages) return (int)(u / kMinPages);
+  // the last w with total * w / kGroups < u + 1
+  return (int)(((u + 1) * kGroups + total - 1) / total) - 1;
+}
+
+// Sum over the lanes up to this one.
+__device__ __forceinline__ unsigned lanes_sum(unsigned v) {
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);   // across rows of 16
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
+  return v;
 }
 
 // Pages of an item: a request's blocks (every KV head and head tile reads as
@@ -131,6 +148,140 @@ __device__ __forceinline__ int v_swz(int r, int c) {
                   : (c ^ ((((r >> 1) & 1) | (((r >> 3) & 1) << 1)) << 1));
 }
 
+// What workgroups hand to each other goes past the XCD's L2, which the others do
+// not see, as agent-scope atomic accesses of 8 bytes: fences would write back and
+// invalidate the whole L2 under the workgroups that still stream (one 128K
+// request: 139 us with them).
+__device__ __forceinline__ void put2(float* p, float x, float y) {
+  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p),
+                     (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x),
+                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get2(const float* p) {
+  const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p),
+                                                 __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+
+// Joins the row whose first piece is workgroup w0's and whose last is w1's, if
+// all of them are there.  Called by every workgroup that has left a piece, after
+// that piece has arrived: the last to arrive finds all the others, so one at least
+// joins the row.  Two may, if they arrive together; they write the same bytes (the
+// pieces are taken in order).
+struct JoinSpace {   // in LDS
+  float4 sums[kThreads];
+  float weight[kGroups][kTileHeads];
+  float part[2][kWaves][kTileHeads];
+  int all;
+};
+template <int D>
+__device__ __forceinline__ void join_row(const DecodeArgs& a, int w0, int w1, long long row, int heads,
+                                         JoinSpace& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = tid & 15;
+  auto slot_of = [&](int e) { return 2 * e + (e == w0 ? 1 : 0); };
+  if (tid < kWave) {
+    bool all = true;
+    for (int e = w0 + lane; e <= w1; e += kWave)
+      all = all && __hip_atomic_load(a.arrived + slot_of(e), __ATOMIC_RELAXED,
+                                     __HIP_MEMORY_SCOPE_AGENT) == a.tag;
+    all = __ballot(!all) == 0;
+    if (lane == 0) s.all = all;
+  }
+  __syncthreads();
+  if (!s.all) return;
+  // nobody waits for these any more; the next launch finds them cleared
+  if (tid < kWave)
+    for (int e = w0 + lane; e <= w1; e += kWave)
+      __hip_atomic_store(a.arrived + slot_of(e), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const int pieces = w1 - w0 + 1;
+  // a thread takes one head's maximum and sum of every 32nd piece, and one of the
+  // n float4 of every lots-th piece
+  constexpr int kEach = kGroups * kTileHeads / kThreads;
+  float2 ml[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int e = (kThreads / kTileHeads) * k + tid / kTileHeads;
+    ml[k] = make_float2(-INFINITY, 0.f);
+    if (e < pieces) ml[k] = get2(a.part_ml + 2 * (slot_of(w0 + e) * kTileHeads + col));
+  }
+  const int n = heads * (D / 4), lots = kThreads / n, lot = tid / n, at = tid - lot * n;
+  auto piece = [&](int e) {
+    const float* const from = a.part_o + (long long)slot_of(w0 + e) * (kTileHeads * D) + 4 * at;
+    const float2 x = get2(from), y = get2(from + 2);
+    return make_float4(x.x, x.y, y.x, y.y);
+  };
+  constexpr int kAhead = 8;
+  float4 x[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int e = lot + lots * k;
+    x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (lot < lots && e < pieces) x[k] = piece(e);
+  }
+  float top = ml[0].x;
+#pragma unroll
+  for (int k = 1; k < kEach; ++k) top = max2(top, ml[k].x);
+  top = groups_max(top);
+  if (lane < kTileHeads) s.part[0][wv][col] = top;
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) top = max2(top, s.part[0][v][col]);
+  const float base = top == -INFINITY ? 0.f : top;
+  float all = 0.f;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int e = (kThreads / kTileHeads) * k + tid / kTileHeads;
+    const float c = fast_exp2(ml[k].x - base);
+    if (e < pieces) s.weight[e][col] = c;
+    all += c * ml[k].y;
+  }
+  all = groups_sum(all);
+  if (lane < kTileHeads) s.part[1][wv][col] = all;
+  __syncthreads();
+  if (tid < heads && a.l.lse) {
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) sum += s.part[1][v][col];
+    a.l.lse[row + col] = sum > 0.f ? (top + __log2f(sum)) * kLn2 : -INFINITY;
+  }
+  const int head = at / (D / 4);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](int e, const float4& y) {
+    const float c = s.weight[e][head];
+    acc.x += c * y.x, acc.y += c * y.y, acc.z += c * y.z, acc.w += c * y.w;
+  };
+  if (lot < lots) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (lot + lots * k < pieces) add(lot + lots * k, x[k]);
+#pragma unroll 8
+    for (int e = lot + lots * kAhead; e < pieces; e += lots) add(e, piece(e));
+    s.sums[tid] = acc;
+  }
+  __syncthreads();
+  if (tid >= n) return;
+  for (int e = 1; e < lots; ++e) {
+    const float4 y = s.sums[e * n + tid];
+    acc.x += y.x, acc.y += y.y, acc.z += y.z, acc.w += y.w;
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) sum += s.part[1][v][head];
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;   // sum is NaN after a score of NaN or +inf
+  reinterpret_cast<u32x2*>(a.l.out + row * D)[tid] =
+      u32x2{pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)};
+}
+
+// A row's pages in a wave's share: pages p .. p + cnt - 1 of its n.
+struct Part {
+  int item, sub, n, p, cnt;
+  int row, heads;        // first output head (b * Hq + head), heads
+  int nkb, last_keys;    // the request's blocks, keys of the last
+  const int32_t* table;  // the page ids of its KV head
+  const int32_t* list;   // its table row's entries, nullptr: every block
+  long long item_start;  // the item's first page
+};
+
 // VT: transposed V pages.  DUP: at most 8 heads per tile, see above.
 template <int D, bool VT, bool DUP>
 __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a) {
@@ -141,116 +292,150 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
   static_assert(kFrag * 16 >= kStage, "");
   __shared__ __align__(16) float4 s_frag[kWaves][2][kFrag];   // [1] is the V stage until the end
   __shared__ float2 s_ml[kWaves][2][kTileHeads];
-  __shared__ int4 s_meta[kWaves][2];   // item, sub, 1 starts | 2 ends, 1 valid
-  __shared__ long long s_sum[kWaves], s_base[kWaves];
-  __shared__ int s_item[kWaves];
+  __shared__ int4 s_meta[kWaves][2];   // row, heads, 1 starts | 2 ends | 4 valid
+  __shared__ long long s_row[kWaves][2][2];   // the piece's row's first and last page
+  static_assert(sizeof(s_frag) >= sizeof(JoinSpace), "");
   const DecodeLaunch& l = a.l;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, grp = lane >> 4;
   const int w = blockIdx.x;
 
-  // ---- shares: prefix sums of the items' pages --------------------------
-  const int per = (a.items + kThreads - 1) / kThreads;
-  const int i0 = tid * per < a.items ? tid * per : a.items;
-  const int i1 = i0 + per < a.items ? i0 + per : a.items;
-  long long mine = 0;
-  for (int i = i0; i < i1; ++i) mine += item_pages(a, i);
-  long long incl = mine;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const long long t = __shfl_up(incl, o, kWave);
-    if (lane >= o) incl += t;
-  }
-  if (lane == 63) s_sum[wv] = incl;
-  if (lane < 2) s_meta[wv][lane].w = 0;
-  __syncthreads();
-  long long before = 0, total = 0;
-#pragma unroll
-  for (int v = 0; v < kWaves; ++v) {
-    if (v < wv) before += s_sum[v];
-    total += s_sum[v];
-  }
-  total = uniform64(total) * a.per_item;
-  const long long u0 = share_start(total, w), u1 = share_start(total, w + 1), nu = u1 - u0;
-  {
-    long long at = (before + incl - mine) * a.per_item;
-    const long long end = (before + incl) * a.per_item;
-    if (end > u0 && at < u1) {
-      for (int i = i0; i < i1; ++i) {
-        const long long next = per == 1 ? end : at + (long long)item_pages(a, i) * a.per_item;
-#pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
-          const long long s = u0 + nu * v / kWaves;
-          if (s >= at && s < next) s_item[v] = i, s_base[v] = at;
+  // ---- this wave's share ---------------------------------------------------
+  // Sums of the items' pages, `per` of them to a lane; every wave makes them by
+  // itself, in registers, which is quicker than to wait for the others.
+  const int per = (a.items + kWave - 1) / kWave;
+  unsigned mine = 0;
+  for (int i = lane * per; i < (lane + 1) * per; ++i)
+    if (i < a.items) mine += item_pages(a, i);
+  const unsigned incl = lanes_sum(mine);
+  const long long total = (long long)(unsigned)__builtin_amdgcn_readlane((int)incl, 63) * a.per_item;
+  auto pages_of = [&](int i) -> int {
+    return per == 1 ? __builtin_amdgcn_readlane((int)mine, i) : uniform(item_pages(a, i));
+  };
+  const long long u0 = share_start(total, w), nu = share_start(total, w + 1) - u0;
+  const long long my0 = u0 + nu * wv / kWaves, my1 = u0 + nu * (wv + 1) / kWaves;
+  if (lane < 2) s_meta[wv][lane].z = 0;
+
+  // ---- its pages, row by row ------------------------------------------------
+  int rem = (int)(my1 - my0);
+  int item = 0, sub = 0, n = 0, p = 0;
+  long long item_start = 0;   // first page of the item
+  if (rem > 0) {
+    // the item with excl <= my0 / per_item < incl
+    unsigned at = (unsigned)((double)my0 / (double)a.per_item);
+    if ((long long)at * a.per_item > my0) --at;
+    else if ((long long)(at + 1) * a.per_item <= my0) ++at;
+    const int found = __builtin_ctzll(__ballot(incl - mine <= at && at < incl));
+    unsigned start = __builtin_amdgcn_readlane((int)(incl - mine), found);
+    item = found * per;
+    n = pages_of(item);
+    if (per > 1) {   // among the lane's items, 64 at a time
+      for (int i = item;; i += kWave) {
+        const unsigned here = i + lane < a.items ? item_pages(a, i + lane) : 0;
+        const unsigned sums = start + lanes_sum(here);
+        const unsigned long long hit = __ballot(sums - here <= at && at < sums);
+        if (hit) {
+          const int k = __builtin_ctzll(hit);
+          item = i + k;
+          n = __builtin_amdgcn_readlane((int)here, k);
+          start = __builtin_amdgcn_readlane((int)(sums - here), k);
+          break;
         }
-        at = next;
+        start = __builtin_amdgcn_readlane((int)sums, 63);
+        if (i + kWave >= a.items) {   // only if the lengths changed under the kernel
+          rem = 0;
+          break;
+        }
       }
     }
+    item_start = (long long)start * a.per_item;
+    const unsigned off = (unsigned)(my0 - item_start);
+    if (n > 0) {
+      sub = (int)(off / (unsigned)n);
+      sub = sub < a.per_item ? sub : a.per_item - 1;
+      p = (int)(off % (unsigned)n);
+    }
   }
-  __syncthreads();
-  const long long my0 = u0 + nu * wv / kWaves, my1 = u0 + nu * (wv + 1) / kWaves;
-
-  // ---- this wave's pages, row by row --------------------------------------
-  int rem = (int)(my1 - my0);   // at most B * Hq * 16384 / 2048
-  int item = 0, sub = 0, n = 0, p = 0;
-  if (rem > 0) {
-    item = uniform(s_item[wv]);
-    const unsigned off = (unsigned)(my0 - uniform64(s_base[wv]));
-    n = uniform(item_pages(a, item));
-    sub = (int)(off / (unsigned)n);
-    p = (int)(off - (unsigned)sub * (unsigned)n);
-  }
+  auto part_of = [&](int item, int sub, int n, int p, int left, long long item_start) {
+    Part t;
+    t.item = item, t.sub = sub, t.n = n, t.p = p, t.item_start = item_start;
+    t.cnt = left < n - p ? left : n - p;
+    int b, g, ht;
+    if (l.kv_indptr) b = item / a.G, g = item - b * a.G, ht = sub;
+    else b = item, g = sub / a.HT, ht = sub - g * a.HT;
+    const int kvh = (int)((long long)g * l.group_size / (a.Hq / a.Hkv));
+    t.row = b * a.Hq + g * l.group_size + ht * kTileHeads;
+    t.heads = l.group_size - ht * kTileHeads;
+    t.heads = t.heads < kTileHeads ? t.heads : kTileHeads;
+    const int len = uniform(request_len(a, b));
+    t.nkb = blocks_for(len);
+    t.last_keys = len - (t.nkb - 1) * kPage;
+    t.table = l.page_table + ((long long)b * a.Hkv + kvh) * a.max_kv_blocks;
+    t.list = l.kv_indptr ? l.kv_indices + uniform(l.kv_indptr[item]) : nullptr;
+    return t;
+  };
+  // the row after t in a share with `left` more pages
+  auto part_after = [&](const Part& t, int left) {
+    int item = t.item, sub = t.sub + 1, n = t.n;
+    long long item_start = t.item_start;
+    if (sub == a.per_item) {
+      sub = 0;
+      item_start += (long long)n * a.per_item;
+      do n = ++item < a.items ? pages_of(item) : -1; while (n == 0);
+      if (n < 0) item = t.item, n = 1;   // only if the lengths changed under the kernel
+    }
+    return part_of(item, sub, n, 0, left, item_start);
+  };
+  // ids of 64 of its pages from `at` on, one per lane: -1 where there is no page
+  // to read, the sign bit set at the request's last block (num_pages < 2^31)
+  auto fetch_ids = [&](const Part& t, int at) {
+    int id = -1;
+    if (at + lane < t.cnt) {
+      const int j = t.list ? t.list[t.p + at + lane] : t.p + at + lane;
+      if (j >= 0 && j < t.nkb) {
+        const int page = t.table[j];
+        if (page >= 0 && page < a.num_pages) id = j == t.nkb - 1 ? page | INT32_MIN : page;
+      }
+    }
+    return id;
+  };
   // element offsets of the lane's loads in a page
   const uint32_t k_off = (uint32_t)((8 * (col >> 2) + (col & 3)) * D + 8 * grp);
   const uint32_t v_off = VT ? (uint32_t)(col * kPage + 8 * grp) : (uint32_t)(lane * 8);
   char* const stage = reinterpret_cast<char*>(&s_frag[wv][1][0]);
 
-  while (rem > 0) {
-    const int cnt = rem < n - p ? rem : n - p;
-    const bool starts = p == 0, ends = p + cnt == n;
-    int b, g, ht;
-    if (l.kv_indptr) b = item / a.G, g = item - b * a.G, ht = sub;
-    else b = item, g = sub / a.HT, ht = sub - g * a.HT;
-    const int kvh = (int)((long long)g * l.group_size / (a.Hq / a.Hkv));
-    const int h0 = g * l.group_size + ht * kTileHeads;
-    int heads = l.group_size - ht * kTileHeads;
-    heads = heads < kTileHeads ? heads : kTileHeads;
-    const int len = uniform(request_len(a, b)), nkb = blocks_for(len);
-    const int32_t* const table = l.page_table + ((long long)b * a.Hkv + kvh) * a.max_kv_blocks;
-    const int32_t* const list = l.kv_indptr ? l.kv_indices + l.kv_indptr[item] : nullptr;
-
-    // ids of 64 pages at a time, one per lane; keys: how many of a page count
-    int ids, keys_of, next_ids = 0, next_keys = 0;
-    auto fetch_ids = [&](int at, int& id, int& keys) {
-      id = 0, keys = 0;
-      if (at + lane < cnt) {
-        const int j = list ? list[p + at + lane] : p + at + lane;
-        if (j >= 0 && j < nkb) {
-          const int page = table[j];
-          if (page >= 0 && page < a.num_pages) {
-            id = page;
-            keys = len - j * kPage < kPage ? len - j * kPage : kPage;
-          }
-        }
-      }
-    };
-    fetch_ids(0, ids, keys_of);
-
+  Part cur = {}, nxt = {};
+  int ids = -1, next_ids = -1, nxt_ids = -1;
+  if (rem > 0) {
+    cur = part_of(item, sub, n, p, rem, item_start);
+    ids = fetch_ids(cur, 0);
+  }
+  // the ids of all waves are asked for before any wave's pages: behind the
+  // pages of 8 waves they come some 10 us later
+  __syncthreads();
+  if (rem > 0) {
+    rem -= cur.cnt;
+    if (rem > 0) {
+      nxt = part_after(cur, rem);
+      nxt_ids = fetch_ids(nxt, 0);
+    }
     bf16x8 q[NK];
-    {
+    auto load_q = [&](const Part& t) {
       const int head = DUP ? (col & 7) : col;
-      const uint16_t* src = l.q + ((long long)b * a.Hq + h0 + head) * D + 8 * grp;
+      const uint16_t* src = l.q + ((long long)t.row + head) * D + 8 * grp;
 #pragma unroll
       for (int s = 0; s < NK; ++s) {
         u32x4 x = {0, 0, 0, 0};
-        if (head < heads) x = *reinterpret_cast<const u32x4*>(src + 32 * s);
+        if (head < t.heads) x = *reinterpret_cast<const u32x4*>(src + 32 * s);
         q[s] = __builtin_bit_cast(bf16x8, x);
       }
-    }
+    };
     u32x4 k[4][NK], v[NL];
+    // a page that is not there: page 0 is read in its place and counts for nothing
+    auto place = [&](int id) { return (long long)(id == -1 ? 0 : id & INT32_MAX) * (kPage * D); };
     auto load_k = [&](int id) {
-      const uint16_t* page = l.k_pool + (long long)id * (kPage * D);
+      const uint16_t* page = l.k_pool + place(id);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -258,26 +443,32 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
           k[t][s] = *reinterpret_cast<const u32x4*>(page + k_off + key_of(t, 0) * D + 32 * s);
     };
     auto load_v = [&](int id) {
-      const uint16_t* page = l.v_pool + (long long)id * (kPage * D);
+      const uint16_t* page = l.v_pool + place(id);
 #pragma unroll
       for (int m = 0; m < NL; ++m)   // VT: d tile m / 2, 32-key step m % 2
         v[m] = *reinterpret_cast<const u32x4*>(
             page + v_off + (VT ? 16 * kPage * (m >> 1) + 32 * (m & 1) : 512 * m));
     };
     f32x4 o[NX];
+    float m, sum;   // m: of q.k, before the scale
+    auto clear = [&] {
 #pragma unroll
-    for (int x = 0; x < NX; ++x) o[x] = {0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, sum = 0.f;   // m: of q.k, before the scale
+      for (int x = 0; x < NX; ++x) o[x] = {0.f, 0.f, 0.f, 0.f};
+      m = -INFINITY, sum = 0.f;
+    };
+    clear();
 
-    int id = __builtin_amdgcn_readlane(ids, 0), keys = __builtin_amdgcn_readlane(keys_of, 0);
+    int id = __builtin_amdgcn_readlane(ids, 0);
+    load_q(cur);
     load_k(id);
     load_v(id);
-    for (int i = 0; i < cnt; ++i) {
-      if ((i & 63) == 0) fetch_ids(i + 64, next_ids, next_keys);
-      int id2 = 0, keys2 = 0;
-      if ((i & 63) == 63) ids = next_ids, keys_of = next_keys;
-      id2 = __builtin_amdgcn_readlane(ids, (i + 1) & 63);
-      keys2 = __builtin_amdgcn_readlane(keys_of, (i + 1) & 63);
+    for (int i = 0;;) {
+      // the next page, of this row or of the next
+      const bool row_done = i + 1 == cur.cnt, go = !row_done || rem > 0;
+      if ((i & 63) == 0) next_ids = fetch_ids(cur, i + 64);
+      if ((i & 63) == 63) ids = next_ids;
+      const int id2 = row_done ? __builtin_amdgcn_readlane(nxt_ids, 0)
+                               : __builtin_amdgcn_readlane(ids, (i + 1) & 63);
       f32x4 s[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) s[t] = {0.f, 0.f, 0.f, 0.f};
@@ -288,9 +479,13 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
           s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][c]), q[c],
                                                          s[t], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
-      if (i + 1 < cnt) load_k(id2);
+      if (go) {
+        if (row_done) load_q(nxt);
+        load_k(id2);
+      }
       __builtin_amdgcn_sched_barrier(0);
-      if (keys < kPage) {   // the last page, or one that is not there
+      if (id < 0) {   // the last page, or one that is not there
+        const int keys = id == -1 ? 0 : cur.last_keys;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -374,115 +569,145 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (i + 1 < cnt) load_v(id2);
-      keys = keys2;
-    }
+      if (go) load_v(id2);
+      id = id2;
+      ++i;
+      if (!row_done) continue;
 
-    sum = groups_sum(sum);
-    if constexpr (DUP)
-#pragma unroll
-      for (int x = 0; x < NX; ++x)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[x][e] += other_half(o[x][e]);
-    const float ml = m * a.scale_log2;
-    if (starts && ends) {
-      if (col < heads) {
-        const long long row = (long long)b * a.Hq + h0 + col;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;   // sum is NaN after a score of NaN or +inf
+      // ---- the row's end, or the share's
+      sum = groups_sum(sum);
+      if constexpr (DUP)
 #pragma unroll
         for (int x = 0; x < NX; ++x)
-          *reinterpret_cast<u32x2*>(l.out + row * D + 16 * x + 4 * grp) =
-              u32x2{pack_bf16x2(o[x][0] * inv, o[x][1] * inv), pack_bf16x2(o[x][2] * inv, o[x][3] * inv)};
-        if (l.lse && grp == 0) l.lse[row] = sum > 0.f ? (ml + __log2f(sum)) * kLn2 : -INFINITY;
-      }
-    } else {
-      const int f = starts ? 1 : 0;   // [1] is the wave's last: its stage is free
 #pragma unroll
-      for (int x = 0; x < NX; ++x)
-        s_frag[wv][f][64 * x + lane] = make_float4(o[x][0], o[x][1], o[x][2], o[x][3]);
-      if (grp == 0) s_ml[wv][f][col] = make_float2(ml, sum);
-      if (lane == 0) s_meta[wv][f] = make_int4(item, sub, (starts ? 1 : 0) | (ends ? 2 : 0), 1);
-    }
-    rem -= cnt;
-    p = 0;
-    if (rem > 0 && ++sub == a.per_item) {
-      sub = 0;
-      do n = ++item < a.items ? uniform(item_pages(a, item)) : -1; while (n == 0);
-      if (n < 0) break;   // only if the lengths changed under the kernel
+          for (int e = 0; e < 4; ++e) o[x][e] += other_half(o[x][e]);
+      const float ml = m * a.scale_log2;
+      const bool starts = cur.p == 0, ends = cur.p + cur.cnt == cur.n;
+      if (starts && ends) {
+        if (col < cur.heads) {
+          const long long row = (long long)cur.row + col;
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;   // sum is NaN after a score of NaN or +inf
+#pragma unroll
+          for (int x = 0; x < NX; ++x)
+            *reinterpret_cast<u32x2*>(l.out + row * D + 16 * x + 4 * grp) =
+                u32x2{pack_bf16x2(o[x][0] * inv, o[x][1] * inv), pack_bf16x2(o[x][2] * inv, o[x][3] * inv)};
+          if (l.lse && grp == 0) l.lse[row] = sum > 0.f ? (ml + __log2f(sum)) * kLn2 : -INFINITY;
+        }
+      } else {
+        const int f = starts ? 1 : 0;   // [1] is the wave's last: its stage is free
+#pragma unroll
+        for (int x = 0; x < NX; ++x)
+          s_frag[wv][f][64 * x + lane] = make_float4(o[x][0], o[x][1], o[x][2], o[x][3]);
+        if (grp == 0) s_ml[wv][f][col] = make_float2(ml, sum);
+        if (lane == 0) {
+          s_meta[wv][f] = make_int4(cur.row, cur.heads, (starts ? 1 : 0) | (ends ? 2 : 0) | 4, 0);
+          s_row[wv][f][0] = cur.item_start + (long long)cur.sub * cur.n;
+          s_row[wv][f][1] = cur.item_start + (long long)(cur.sub + 1) * cur.n - 1;
+        }
+      }
+      if (!go) break;
+      clear();
+      cur = nxt;
+      ids = nxt_ids;
+      i = 0;
+      rem -= cur.cnt;
+      if (rem > 0) {
+        nxt = part_after(cur, rem);
+        nxt_ids = fetch_ids(nxt, 0);
+      }
     }
   }
   __syncthreads();
 
   // ---- the waves' pieces, row by row -----------------------------------------
-  long long row_end = 0;
-  int next_row = 0, next_heads = 0;
-  for (int f = 0; f < 2 * kWaves;) {
-    const int4 meta = s_meta[f >> 1][f & 1];
-    if (!meta.w) {
-      ++f;
-      continue;
-    }
-    int last = f, flags = meta.z;
-    for (int e = f + 1; e < 2 * kWaves; ++e) {
-      const int4 other = s_meta[e >> 1][e & 1];
-      if (!other.w) continue;
-      if (other.x != meta.x || other.y != meta.y) break;
-      last = e;
-      flags |= other.z & 2;
-    }
-    int b, g, ht;
-    if (l.kv_indptr) b = meta.x / a.G, g = meta.x - b * a.G, ht = meta.y;
-    else b = meta.x, g = meta.y / a.HT, ht = meta.y - g * a.HT;
-    const int h0 = g * l.group_size + ht * kTileHeads;
-    int heads = l.group_size - ht * kTileHeads;
-    heads = heads < kTileHeads ? heads : kTileHeads;
-    const long long row = (long long)b * a.Hq + h0 + col;
-    if (wv < NX) {
-      float top = -INFINITY, all = 0.f;
-      for (int e = f; e <= last; ++e)
-        if (s_meta[e >> 1][e & 1].w) top = max2(top, s_ml[e >> 1][e & 1][col].x);
+  // In page order they are piece 2 v + f of wave v; one that does not start a row
+  // goes on with the row of the piece before it, so a row has one of a wave at most.
+  // Rows that other workgroups share: [0] the one before the share, [1] behind it.
+  int left_w0[2] = {-1, -1}, left_w1[2] = {0, 0}, left_heads[2] = {0, 0}, left_row[2] = {0, 0};
+  int4 meta = make_int4(0, 0, 0, 0);
+  if (lane < 2 * kWaves) meta = s_meta[lane >> 1][lane & 1];
+  const unsigned valid = (unsigned)__ballot((meta.z & 4) != 0);
+  const unsigned starting = (unsigned)__ballot((meta.z & 5) == 5);
+  const unsigned ending = (unsigned)__ballot((meta.z & 6) == 6);
+  for (unsigned rest = valid; rest;) {
+    const int f = __builtin_ctz(rest);
+    const unsigned next = starting & rest & ~((2u << f) - 1);
+    const unsigned set = rest & (next ? (next & (0u - next)) - 1 : ~0u);
+    rest &= ~set;
+    const int last = 31 - __builtin_clz(set);
+    const int flags = ((starting >> f) & 1) | (((ending >> last) & 1) << 1);
+    const int row = __builtin_amdgcn_readlane(meta.x, f), heads = __builtin_amdgcn_readlane(meta.y, f);
+    for (int x = wv; x < NX; x += kWaves) {
+      float2 ml[kWaves];
+      float4 o[kWaves];
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {   // a wave without a piece: the first piece, not counted
+        const unsigned has = (set >> (2 * v)) & 3;
+        const int at = has ? 2 * v + (int)(has >> 1) : f;
+        ml[v] = s_ml[at >> 1][at & 1][col];
+        o[v] = s_frag[at >> 1][at & 1][64 * x + lane];
+      }
+      float top = ml[0].x;
+#pragma unroll
+      for (int v = 1; v < kWaves; ++v) top = max2(top, ml[v].x);
       const float base = top == -INFINITY ? 0.f : top;
+      float all = 0.f;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int e = f; e <= last; ++e) {
-        if (!s_meta[e >> 1][e & 1].w) continue;
-        const float2 ml = s_ml[e >> 1][e & 1][col];
-        const float4 x = s_frag[e >> 1][e & 1][64 * wv + lane];
-        const float c = fast_exp2(ml.x - base);
-        all += c * ml.y;
-        acc.x += c * x.x, acc.y += c * x.y, acc.z += c * x.z, acc.w += c * x.w;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        const float c = ((set >> (2 * v)) & 3) ? fast_exp2(ml[v].x - base) : 0.f;
+        all += c * ml[v].y;
+        acc.x += c * o[v].x, acc.y += c * o[v].y, acc.z += c * o[v].z, acc.w += c * o[v].w;
       }
-      if (flags == 3) {
-        if (col < heads) {
+      if (col < heads) {
+        const int d = 16 * x + 4 * grp;
+        if (flags == 3) {
           const float inv = all == 0.f ? 0.f : 1.f / all;
-          *reinterpret_cast<u32x2*>(l.out + row * D + 16 * wv + 4 * grp) =
+          *reinterpret_cast<u32x2*>(l.out + ((long long)row + col) * D + d) =
               u32x2{pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)};
-          if (l.lse && wv == 0 && grp == 0)
-            l.lse[row] = all > 0.f ? (top + __log2f(all)) * kLn2 : -INFINITY;
+          if (l.lse && x == 0 && grp == 0)
+            l.lse[row + col] = all > 0.f ? (top + __log2f(all)) * kLn2 : -INFINITY;
+        } else {
+          const int slot = 2 * w + (flags & 1);
+          float* const to = a.part_o + ((long long)slot * kTileHeads + col) * D + d;
+          put2(to, acc.x, acc.y);
+          put2(to + 2, acc.z, acc.w);
+          if (x == 0 && grp == 0) put2(a.part_ml + 2 * (slot * kTileHeads + col), top, all);
         }
-      } else {   // [1]: the row starts here and goes on; [0]: it started before
-        const int slot = 2 * w + (flags & 1);
-        a.part_o[(long long)slot * kFrag + 64 * wv + lane] = acc;
-        if (wv == 0 && grp == 0) a.part_ml[slot * kTileHeads + col] = make_float2(top, all);
       }
     }
-    if (flags == 1 && tid == 0) {
-      // where the row ends: its item's first page, and the rows of the item before it
-      const int v = last >> 1;
-      const int pages = item_pages(a, meta.x);
-      long long base = s_base[v];
-      // s_base is of the item that wave v starts in; walk to the piece's
-      for (int i = s_item[v]; i < meta.x; ++i) base += (long long)item_pages(a, i) * a.per_item;
-      row_end = base + (long long)(meta.y + 1) * pages;
-      next_row = (int)((long long)b * a.Hq + h0);
-      next_heads = heads;
+    if (flags != 3) {
+      const int side = flags & 1;
+      const int w0 = share_of(total, uniform64(s_row[f >> 1][f & 1][0]));
+      const int w1 = share_of(total, uniform64(s_row[f >> 1][f & 1][1]));
+      if (side) left_w0[1] = w0, left_w1[1] = w1, left_heads[1] = heads, left_row[1] = row;
+      else left_w0[0] = w0, left_w1[0] = w1, left_heads[0] = heads, left_row[0] = row;
     }
-    f = last + 1;
   }
-  if (tid == 0) a.shares[w] = Share{row_end, total, next_row, next_heads};
+  if (left_w0[0] >= 0 || left_w0[1] >= 0) {
+    // a piece counts as arrived once every wave's stores of it are done; the
+    // swap is done when its answer is there, and only then are the others' read
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (tid < 2 && (tid == 0 ? left_w0[0] : left_w0[1]) >= 0) {
+      const unsigned long long was = __hip_atomic_exchange(a.arrived + 2 * w + tid, a.tag,
+                                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("" : : "v"(was) : "memory");
+      __builtin_amdgcn_s_waitcnt(0);
+    }
+    JoinSpace& space = *reinterpret_cast<JoinSpace*>(&s_frag[0][0][0]);
+#pragma unroll
+    for (int side = 0; side < 2; ++side)
+      if (left_w0[side] >= 0) {
+        __syncthreads();   // the LDS of the row before
+        join_row<D>(a, left_w0[side], left_w1[side], left_row[side], left_heads[side], space);
+      }
+  }
 
   // ---- requests and rows without a page -----------------------------------
   for (int i = w; i < a.items; i += kGroups) {
-    if (item_pages(a, i) > 0) continue;
+    if (pages_of(i) > 0) continue;
     const int nh = a.Hq / (l.kv_indptr ? a.G : 1);
     const long long row = l.kv_indptr ? (long long)(i / a.G) * a.Hq + (long long)(i % a.G) * nh
                                       : (long long)i * a.Hq;
@@ -493,60 +718,30 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
   }
 }
 
-// Rows that several workgroups share: workgroup (w, x) joins d tile x of the
-// row that starts in share w and goes on after it; its waves take the pieces in
-// turn, and are joined in LDS.
-template <int D>
-__global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs a) {
-  constexpr int kFrag = D / 16 * 64;
-  __shared__ float4 s_o[kWaves][64];
-  __shared__ float2 s_ml[kWaves][kTileHeads];
-  const int w = blockIdx.x, x = blockIdx.y;
-  const Share s = a.shares[w];
-  if (s.row_end == 0) return;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
-  float top = -INFINITY, all = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](float2 ml, float4 o) {
-    const float mn = max2(top, ml.x), base = mn == -INFINITY ? 0.f : mn;
-    const float c0 = fast_exp2(top - base), c1 = fast_exp2(ml.x - base);
-    all = all * c0 + ml.y * c1;
-    acc.x = acc.x * c0 + o.x * c1, acc.y = acc.y * c0 + o.y * c1;
-    acc.z = acc.z * c0 + o.z * c1, acc.w = acc.w * c0 + o.w * c1;
-    top = mn;
-  };
-  for (int e = w + wv; e < kGroups && (e == w || share_start(s.total, e) < s.row_end); e += kWaves) {
-    const int slot = 2 * e + (e == w ? 1 : 0);
-    add(a.part_ml[slot * kTileHeads + col], a.part_o[(long long)slot * kFrag + 64 * x + lane]);
-  }
-  s_o[wv][lane] = acc;
-  if (grp == 0) s_ml[wv][col] = make_float2(top, all);
-  __syncthreads();
-  if (wv > 0) return;
-  for (int e = 1; e < kWaves; ++e) add(s_ml[e][col], s_o[e][lane]);
-  if (col >= s.heads) return;
-  const long long row = (long long)s.out_row + col;
-  const float inv = all == 0.f ? 0.f : 1.f / all;
-  *reinterpret_cast<u32x2*>(a.l.out + row * D + 16 * x + 4 * grp) =
-      u32x2{pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)};
-  if (a.l.lse && x == 0 && grp == 0)
-    a.l.lse[row] = all > 0.f ? (top + __log2f(all)) * kLn2 : -INFINITY;
-}
-
 template <int D, bool VT>
 hipError_t launch(const DecodeArgs& a, hipStream_t st) {
   if (a.l.group_size <= 8) decode_kernel<D, VT, true><<<kGroups, kThreads, 0, st>>>(a);
   else decode_kernel<D, VT, false><<<kGroups, kThreads, 0, st>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  decode_join_kernel<D><<<dim3(kGroups, D / 16), kThreads, 0, st>>>(a);
   return hipGetLastError();
+}
+
+// A tag per launch: what the workspace held before, an earlier launch's tag among
+// it, does not count as arrived.
+unsigned long long next_tag() {
+  static std::atomic<unsigned long long> next{[] {
+    std::random_device rd;
+    return ((unsigned long long)rd() << 32) ^ rd() ^
+           (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count();
+  }()};
+  const unsigned long long t = next.fetch_add(1, std::memory_order_relaxed);
+  return t != 0 ? t : next_tag();
 }
 
 }  // namespace
 
 size_t decode_ws_bytes(const CacheDims& d, int) {
-  return (size_t)kGroups * (2 * kTileHeads * (d.D * sizeof(float) + sizeof(float2)) + sizeof(Share));
+  return (size_t)kGroups * (2 * kTileHeads * (d.D * sizeof(float) + sizeof(float2)) +
+                           2 * sizeof(unsigned long long));
 }
 
 hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& l, hipStream_t st) {
@@ -562,9 +757,10 @@ hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& l, hipStream_t 
   a.max_kv_blocks = d.max_kv_blocks;
   a.num_pages = d.num_pages;
   a.scale_log2 = l.sm_scale * kLog2e;
-  a.part_o = static_cast<float4*>(l.ws);
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)kGroups * 2 * kTileHeads * d.D / 4);
-  a.shares = reinterpret_cast<Share*>(a.part_ml + (size_t)kGroups * 2 * kTileHeads);
+  a.part_o = static_cast<float*>(l.ws);
+  a.part_ml = a.part_o + (size_t)kGroups * 2 * kTileHeads * d.D;
+  a.arrived = reinterpret_cast<unsigned long long*>(a.part_ml + (size_t)kGroups * 2 * kTileHeads * 2);
+  a.tag = next_tag();
   const bool vt = d.v_layout != 0;
   if (d.D == 64) return vt ? launch<64, true>(a, st) : launch<64, false>(a, st);
   return vt ? launch<128, true>(a, st) : launch<128, false>(a, st);
