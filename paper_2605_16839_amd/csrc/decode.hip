@@ -27,6 +27,7 @@
 #include <chrono>
 #include <cstdint>
 #include <random>
+#include <type_traits>
 
 #include "common.hpp"
 #include "serving.hpp"
@@ -138,12 +139,21 @@ typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 constexpr int key_of(int kt, int r) {
   return 32 * (kt >> 1) + 8 * (r >> 2) + 4 * (kt & 1) + (r & 3);
 }
-// 16-byte chunk where chunk c of row r of a token-major V tile lies: 32 lanes of
-// a transpose read cover keys {0..3, 8..11} (+ multiples) x 32 bytes, so bits 0, 1
-// and 3 of the key pick the 32-byte pair (64-element rows: bit 0 picks the half
-// of the 256-byte bank window).
-template <int D>
-__device__ __forceinline__ int v_swz(int r, int c) {
+// Half a page in LDS: 32 keys of K or token-major V (rows of D), D / 2 rows of a
+// transposed V page (64 keys each).  16-byte chunk where chunk c of row r lies, so
+// that operand reads meet no bank twice:
+//   K: 16 lanes read 16 bytes each, of rows that differ in bits 0, 1, 3 and 4;
+//   token-major V: 32 lanes of a transpose read cover rows {0..3, 8..11} (+
+//     multiples) x 32 bytes, so bits 0, 1 and 3 pick the 32-byte pair;
+//   transposed V: 16 lanes read 16 bytes each, of 16 rows in a row.
+// Where rows are 128 bytes, two share the 256 bytes of all banks, by bit 0.
+enum Half { kHalfK, kHalfV, kHalfVT };
+template <int D, Half H>
+__device__ __forceinline__ int swizzle(int r, int c) {
+  if (H == kHalfVT) return c ^ ((r >> 1) & 7);
+  if (H == kHalfK)
+    return D == 128 ? (c ^ ((r & 3) | (((r >> 3) & 3) << 2)))
+                    : (c ^ (((r >> 1) & 1) | (((r >> 3) & 3) << 1)));
   return D == 128 ? (c ^ (((r & 3) | (((r >> 3) & 1) << 2)) << 1))
                   : (c ^ ((((r >> 1) & 1) | (((r >> 3) & 1) << 1)) << 1));
 }
@@ -196,7 +206,7 @@ __device__ __forceinline__ void join_row(const DecodeArgs& a, int w0, int w1, lo
   const int pieces = w1 - w0 + 1;
   // a thread takes one head's maximum and sum of every 32nd piece, and one of the
   // n float4 of every lots-th piece
-  constexpr int kEach = kGroups * kTileHeads / kThreads;
+  constexpr int kEach = (kGroups * kTileHeads + kThreads - 1) / kThreads;
   float2 ml[kEach];
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
@@ -306,8 +316,14 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
   // itself, in registers, which is quicker than to wait for the others.
   const int per = (a.items + kWave - 1) / kWave;
   unsigned mine = 0;
-  for (int i = lane * per; i < (lane + 1) * per; ++i)
-    if (i < a.items) mine += item_pages(a, i);
+  int my_len = 0;   // of the request, where a lane has one and no tables are given
+  if (per == 1 && !l.kv_indptr) {
+    if (lane < a.items) my_len = request_len(a, lane);
+    mine = blocks_for(my_len);
+  } else {
+    for (int i = lane * per; i < (lane + 1) * per; ++i)
+      if (i < a.items) mine += item_pages(a, i);
+  }
   const unsigned incl = lanes_sum(mine);
   const long long total = (long long)(unsigned)__builtin_amdgcn_readlane((int)incl, 63) * a.per_item;
   auto pages_of = [&](int i) -> int {
@@ -368,7 +384,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
     t.row = b * a.Hq + g * l.group_size + ht * kTileHeads;
     t.heads = l.group_size - ht * kTileHeads;
     t.heads = t.heads < kTileHeads ? t.heads : kTileHeads;
-    const int len = uniform(request_len(a, b));
+    const int len = per == 1 && !l.kv_indptr ? __builtin_amdgcn_readlane(my_len, item)
+                                             : uniform(request_len(a, b));
     t.nkb = blocks_for(len);
     t.last_keys = len - (t.nkb - 1) * kPage;
     t.table = l.page_table + ((long long)b * a.Hkv + kvh) * a.max_kv_blocks;
@@ -400,9 +417,6 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
     }
     return id;
   };
-  // element offsets of the lane's loads in a page
-  const uint32_t k_off = (uint32_t)((8 * (col >> 2) + (col & 3)) * D + 8 * grp);
-  const uint32_t v_off = VT ? (uint32_t)(col * kPage + 8 * grp) : (uint32_t)(lane * 8);
   char* const stage = reinterpret_cast<char*>(&s_frag[wv][1][0]);
 
   Part cur = {}, nxt = {};
@@ -416,10 +430,6 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
   __syncthreads();
   if (rem > 0) {
     rem -= cur.cnt;
-    if (rem > 0) {
-      nxt = part_after(cur, rem);
-      nxt_ids = fetch_ids(nxt, 0);
-    }
     bf16x8 q[NK];
     auto load_q = [&](const Part& t) {
       const int head = DUP ? (col & 7) : col;
@@ -431,23 +441,28 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
         q[s] = __builtin_bit_cast(bf16x8, x);
       }
     };
-    u32x4 k[4][NK], v[NL];
-    // a page that is not there: page 0 is read in its place and counts for nothing
-    auto place = [&](int id) { return (long long)(id == -1 ? 0 : id & INT32_MAX) * (kPage * D); };
-    auto load_k = [&](int id) {
-      const uint16_t* page = l.k_pool + place(id);
+    // A page on its way: whole rows, 1 KB a load.  One page of a wave is in
+    // flight at a time, K(i), V(i), K(i + 1), ..: two (K(i + 1) while V(i) is on its
+    // way) were 14% slower on 5.6 GB, and loads that keep their lines 12%.
+    u32x4 x[NL];
+    auto load = [&](const uint16_t* pool, int id) {
+      // a page that is not there: page 0 is read in its place and counts for nothing
+      const uint16_t* page = pool + (long long)(id == -1 ? 0 : id & INT32_MAX) * (kPage * D);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int s = 0; s < NK; ++s)
-          k[t][s] = *reinterpret_cast<const u32x4*>(page + k_off + key_of(t, 0) * D + 32 * s);
+      for (int y = 0; y < NL; ++y)
+        x[y] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(page + 512 * y + 8 * lane));
+      __builtin_amdgcn_sched_barrier(0);
     };
-    auto load_v = [&](int id) {
-      const uint16_t* page = l.v_pool + place(id);
+    auto to_stage = [&](auto kind, int half) {
+      constexpr Half H = decltype(kind)::value;
+      constexpr int RL = H == kHalfVT ? kPage : D;   // elements of a row
 #pragma unroll
-      for (int m = 0; m < NL; ++m)   // VT: d tile m / 2, 32-key step m % 2
-        v[m] = *reinterpret_cast<const u32x4*>(
-            page + v_off + (VT ? 16 * kPage * (m >> 1) + 32 * (m & 1) : 512 * m));
+      for (int y = 0; y < NL / 2; ++y) {
+        const int e = 512 * y + 8 * lane, r = e / RL, c = (e % RL) / 8;
+        *reinterpret_cast<u32x4*>(stage + r * RL * 2 + 16 * swizzle<D, H>(r, c)) = x[half * (NL / 2) + y];
+      }
+      __builtin_amdgcn_wave_barrier();
     };
     f32x4 o[NX];
     float m, sum;   // m: of q.k, before the scale
@@ -460,8 +475,11 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
 
     int id = __builtin_amdgcn_readlane(ids, 0);
     load_q(cur);
-    load_k(id);
-    load_v(id);
+    load(l.k_pool, id);
+    if (rem > 0) {
+      nxt = part_after(cur, rem);
+      nxt_ids = fetch_ids(nxt, 0);
+    }
     for (int i = 0;;) {
       // the next page, of this row or of the next
       const bool row_done = i + 1 == cur.cnt, go = !row_done || rem > 0;
@@ -473,17 +491,21 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
 #pragma unroll
       for (int t = 0; t < 4; ++t) s[t] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < NK; ++c)
+      for (int h = 0; h < 2; ++h) {
+        to_stage(std::integral_constant<Half, kHalfK>{}, h);
+        if (h == 1) load(l.v_pool, id);
+        const int r0 = 8 * (col >> 2) + (col & 3);
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][c]), q[c],
-                                                         s[t], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      if (go) {
-        if (row_done) load_q(nxt);
-        load_k(id2);
+        for (int c = 0; c < NK; ++c)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const u32x4 f = *reinterpret_cast<const u32x4*>(
+                stage + (r0 + 4 * t) * D * 2 + 16 * swizzle<D, kHalfK>(r0, 4 * c + grp));
+            s[2 * h + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), q[c],
+                                                                   s[2 * h + t], 0, 0, 0);
+          }
+        __builtin_amdgcn_wave_barrier();
       }
-      __builtin_amdgcn_sched_barrier(0);
       if (id < 0) {   // the last page, or one that is not there
         const int keys = id == -1 ? 0 : cur.last_keys;
 #pragma unroll
@@ -491,20 +513,6 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (key_of(t, 0) + 8 * grp + e >= keys) s[t][e] = -INFINITY;
-        // weights of 0 do not undo a NaN in V
-#pragma unroll
-        for (int x = 0; x < NL; ++x) {
-          if constexpr (VT) {
-            const int first = 32 * (x & 1) + 8 * grp;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (first + 2 * e >= keys) v[x][e] = 0;
-              else if (first + 2 * e + 1 >= keys) v[x][e] &= 0xffffu;
-            }
-          } else {
-            if ((512 * x + 8 * lane) / D >= keys) v[x] = {0, 0, 0, 0};
-          }
-        }
       }
       float top = s[0][0];
 #pragma unroll
@@ -537,39 +545,55 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
         }
 #pragma unroll
       for (int x = 0; x < NX; ++x) o[x] *= alpha;
-      if constexpr (VT) {
+      if (id < 0) {
+        const int keys = id == -1 ? 0 : cur.last_keys;
+        // weights of 0 do not undo a NaN in V
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int y = 0; y < NL; ++y) {
+          if constexpr (VT) {
+            const int first = 8 * (lane & 7);
 #pragma unroll
-          for (int x = 0; x < NX; ++x)
-            o[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, v[2 * x + c]), pt[c], o[x], 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-#pragma unroll
-          for (int y = 0; y < NL / 2; ++y) {
-            const int e = 512 * y + 8 * lane, r = e / D, ch = (e % D) / 8;
-            *reinterpret_cast<u32x4*>(stage + r * D * 2 + 16 * v_swz<D>(r, ch)) = v[c * (NL / 2) + y];
+            for (int e = 0; e < 4; ++e) {
+              if (first + 2 * e >= keys) x[y][e] = 0;
+              else if (first + 2 * e + 1 >= keys) x[y][e] &= 0xffffu;
+            }
+          } else {
+            if ((512 * y + 8 * lane) / D >= keys) x[y] = {0, 0, 0, 0};
           }
-          __builtin_amdgcn_wave_barrier();
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        to_stage(std::integral_constant<Half, VT ? kHalfVT : kHalfV>{}, h);
+        if (h == 1 && go) {
+          if (row_done) load_q(nxt);
+          load(l.k_pool, id2);
+        }
+        if constexpr (VT) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int y = 0; y < NX / 2; ++y) {
+              const u32x4 f = *reinterpret_cast<const u32x4*>(
+                  stage + (16 * y + col) * kPage * 2 + 16 * swizzle<D, kHalfVT>(col, 4 * c + grp));
+              f32x4& to = o[h * (NX / 2) + y];
+              to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pt[c], to, 0, 0, 0);
+            }
+        } else {
           const int r0 = 8 * grp + (col >> 2);
 #pragma unroll
-          for (int x = 0; x < NX; ++x) {
-            const int d = 16 * x + 4 * (col & 3);
-            const char* src = stage + r0 * D * 2 + 16 * v_swz<D>(r0, d >> 3) + 2 * (d & 7);
+          for (int y = 0; y < NX; ++y) {
+            const int d = 16 * y + 4 * (col & 3);
+            const char* src = stage + r0 * D * 2 + 16 * swizzle<D, kHalfV>(r0, d >> 3) + 2 * (d & 7);
             const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)src);
             const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 4 * D * 2));
             const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
             const u32x4 f = {l2[0], l2[1], h2[0], h2[1]};
-            o[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pt[c],
-                                                           o[x], 0, 0, 0);
+            o[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pt[h], o[y], 0, 0, 0);
           }
-          __builtin_amdgcn_wave_barrier();
         }
+        __builtin_amdgcn_wave_barrier();
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (go) load_v(id2);
       id = id2;
       ++i;
       if (!row_done) continue;
