@@ -23,10 +23,7 @@
 //   * a row that lies inside one wave's share is written at once; pieces of
 //     a workgroup's waves are joined in its LDS, and rows that several workgroups
 //     share by the last of them (join_row).
-#include <atomic>
-#include <chrono>
 #include <cstdint>
-#include <random>
 #include <type_traits>
 
 #include "common.hpp"
@@ -38,7 +35,8 @@ namespace {
 constexpr int kWaves = 8;                   // per workgroup
 constexpr int kThreads = kWaves * kWave;
 constexpr int kGroups = 256;                // one workgroup per CU
-constexpr int kMinPages = 2 * kWaves;       // of a workgroup's share
+constexpr int kMinPages = 4;                // of a workgroup's share
+constexpr int kFewRows = 8;                 // so many rows at most are joined by a launch of its own
 constexpr int kTileHeads = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -51,8 +49,8 @@ struct DecodeArgs {
   // starts in the middle of, [1] of the row that goes on after its share
   float* part_o;                    // [kGroups][2][16][D]
   float* part_ml;                   // [kGroups][2][16][2]: maximum (log2 units) and sum
-  unsigned long long* arrived;      // [kGroups][2]: tag once a piece is there
-  unsigned long long tag;           // this launch's, never 0
+  unsigned long long* arrived;      // [kGroups]: pieces there are of the row that starts in a share
+  bool join_later;                  // decode_join_kernel joins the rows
 };
 
 template <typename T>
@@ -100,9 +98,11 @@ __device__ __forceinline__ long long share_start(long long total, int w) {
   return s < total ? s : total;
 }
 __device__ __forceinline__ int share_of(long long total, long long u) {
-  if (total < (long long)kGroups * kMinPages) return (int)(u / kMinPages);
-  // the last w with total * w / kGroups < u + 1
-  return (int)(((u + 1) * kGroups + total - 1) / total) - 1;
+  if (total < (long long)kGroups * kMinPages) return (int)u / kMinPages;
+  int w = (int)((float)u / (float)total * kGroups);   // off by one at most
+  w = w < kGroups - 1 ? w : kGroups - 1;
+  if (share_start(total, w) > u) return w - 1;
+  return share_start(total, w + 1) <= u ? w + 1 : w;
 }
 
 // Sum over the lanes up to this one.
@@ -173,36 +173,40 @@ __device__ __forceinline__ float2 get2(const float* p) {
   return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
 
-// Joins the row whose first piece is workgroup w0's and whose last is w1's, if
-// all of them are there.  Called by every workgroup that has left a piece, after
-// that piece has arrived: the last to arrive finds all the others, so one at least
-// joins the row.  Two may, if they arrive together; they write the same bytes (the
-// pieces are taken in order).
+// Counts a piece of a row in; true for the last of n.  A counter is kCounter plus
+// the pieces so far, and plain kCounter between launches.  A workspace may hold
+// anything at first: who finds a value that is no counter makes it one, with a swap
+// that only one of those who find it can win, and counts in if it is another.
+constexpr unsigned long long kCounter = 0x5ca1ab1e'0dd5'0000ull;
+__device__ __forceinline__ bool last_of(unsigned long long* counter, int n) {
+  unsigned long long was =
+      __hip_atomic_fetch_add(counter, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  while ((was ^ kCounter) >> 16) {
+    unsigned long long now = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if ((now ^ kCounter) >> 16) {
+      if (__hip_atomic_compare_exchange_strong(counter, &now, kCounter + 1, __ATOMIC_RELAXED,
+                                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+        was = kCounter;
+    } else {
+      was = __hip_atomic_fetch_add(counter, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  if ((int)(was & 0xffff) != n - 1) return false;
+  __hip_atomic_store(counter, kCounter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
+// Joins the row whose first piece is workgroup w0's and whose last is w1's.
 struct JoinSpace {   // in LDS
   float4 sums[kThreads];
   float weight[kGroups][kTileHeads];
   float part[2][kWaves][kTileHeads];
-  int all;
 };
 template <int D>
 __device__ __forceinline__ void join_row(const DecodeArgs& a, int w0, int w1, long long row, int heads,
                                          JoinSpace& s) {
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, col = tid & 15;
   auto slot_of = [&](int e) { return 2 * e + (e == w0 ? 1 : 0); };
-  if (tid < kWave) {
-    bool all = true;
-    for (int e = w0 + lane; e <= w1; e += kWave)
-      all = all && __hip_atomic_load(a.arrived + slot_of(e), __ATOMIC_RELAXED,
-                                     __HIP_MEMORY_SCOPE_AGENT) == a.tag;
-    all = __ballot(!all) == 0;
-    if (lane == 0) s.all = all;
-  }
-  __syncthreads();
-  if (!s.all) return;
-  // nobody waits for these any more; the next launch finds them cleared
-  if (tid < kWave)
-    for (int e = w0 + lane; e <= w1; e += kWave)
-      __hip_atomic_store(a.arrived + slot_of(e), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   const int pieces = w1 - w0 + 1;
   // a thread takes one head's maximum and sum of every 32nd piece, and one of the
   // n float4 of every lots-th piece
@@ -419,6 +423,12 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
   };
   char* const stage = reinterpret_cast<char*>(&s_frag[wv][1][0]);
 
+  // The waves keep step, a barrier each page, with the next page already on its
+  // way: left alone, some are served first throughout, and end 30 us of 80 before
+  // the others, with too little in flight for the rest (52 ragged requests: 112.4 us
+  // without, 109.7 with).  All take as many barriers as the longest share has pages.
+  int step = 0;
+  const int steps = (int)((nu + kWaves - 1) / kWaves);
   Part cur = {}, nxt = {};
   int ids = -1, next_ids = -1, nxt_ids = -1;
   if (rem > 0) {
@@ -569,6 +579,10 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
           if (row_done) load_q(nxt);
           load(l.k_pool, id2);
         }
+        if (h == 1) {   // see `steps`
+          __builtin_amdgcn_s_barrier();
+          ++step;
+        }
         if constexpr (VT) {
 #pragma unroll
           for (int c = 0; c < 2; ++c)
@@ -641,6 +655,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
       }
     }
   }
+  for (; step < steps; ++step) __builtin_amdgcn_s_barrier();
   __syncthreads();
 
   // ---- the waves' pieces, row by row -----------------------------------------
@@ -653,15 +668,28 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
   const unsigned valid = (unsigned)__ballot((meta.z & 4) != 0);
   const unsigned starting = (unsigned)__ballot((meta.z & 5) == 5);
   const unsigned ending = (unsigned)__ballot((meta.z & 6) == 6);
-  for (unsigned rest = valid; rest;) {
-    const int f = __builtin_ctz(rest);
-    const unsigned next = starting & rest & ~((2u << f) - 1);
-    const unsigned set = rest & (next ? (next & (0u - next)) - 1 : ~0u);
-    rest &= ~set;
+  const unsigned firsts = starting | (valid & (0u - valid));   // the first piece of every row
+  const int rows = __builtin_popcount(firsts);
+  // few rows: several waves to a row, each some of the d tiles
+  const int per_row = rows >= kWaves ? 1 : kWaves / (rows > 0 ? rows : 1);
+  unsigned ahead = firsts;   // without the rows before the one at hand
+  for (int r = 0, at_row = wv / per_row; r < rows; ++r, ahead &= ahead - 1) {
+    const int f = __builtin_ctz(ahead);
+    const unsigned next = ahead & (ahead - 1);
+    const unsigned set = valid & ~((1u << f) - 1) & (next ? (next & (0u - next)) - 1 : ~0u);
     const int last = 31 - __builtin_clz(set);
     const int flags = ((starting >> f) & 1) | (((ending >> last) & 1) << 1);
     const int row = __builtin_amdgcn_readlane(meta.x, f), heads = __builtin_amdgcn_readlane(meta.y, f);
-    for (int x = wv; x < NX; x += kWaves) {
+    if (flags != 3) {
+      const int side = flags & 1;
+      const int w0 = share_of(total, uniform64(s_row[f >> 1][f & 1][0]));
+      const int w1 = share_of(total, uniform64(s_row[f >> 1][f & 1][1]));
+      if (side) left_w0[1] = w0, left_w1[1] = w1, left_heads[1] = heads, left_row[1] = row;
+      else left_w0[0] = w0, left_w1[0] = w1, left_heads[0] = heads, left_row[0] = row;
+    }
+    if (r != at_row) continue;
+    at_row += kWaves / per_row;
+    for (int x = wv % per_row; x < NX; x += per_row) {
       float2 ml[kWaves];
       float4 o[kWaves];
 #pragma unroll
@@ -700,32 +728,24 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
         }
       }
     }
-    if (flags != 3) {
-      const int side = flags & 1;
-      const int w0 = share_of(total, uniform64(s_row[f >> 1][f & 1][0]));
-      const int w1 = share_of(total, uniform64(s_row[f >> 1][f & 1][1]));
-      if (side) left_w0[1] = w0, left_w1[1] = w1, left_heads[1] = heads, left_row[1] = row;
-      else left_w0[0] = w0, left_w1[0] = w1, left_heads[0] = heads, left_row[0] = row;
-    }
   }
-  if (left_w0[0] >= 0 || left_w0[1] >= 0) {
-    // a piece counts as arrived once every wave's stores of it are done; the
-    // swap is done when its answer is there, and only then are the others' read
+  if (!a.join_later && (left_w0[0] >= 0 || left_w0[1] >= 0)) {
+    // a piece counts once every wave's stores of it are done
+    __shared__ int s_last[2];
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (tid < 2 && (tid == 0 ? left_w0[0] : left_w0[1]) >= 0) {
-      const unsigned long long was = __hip_atomic_exchange(a.arrived + 2 * w + tid, a.tag,
-                                                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      asm volatile("" : : "v"(was) : "memory");
-      __builtin_amdgcn_s_waitcnt(0);
+    if (tid < 2) {
+      const int w0 = tid ? left_w0[1] : left_w0[0], w1 = tid ? left_w1[1] : left_w1[0];
+      s_last[tid] = w0 >= 0 && last_of(a.arrived + w0, w1 - w0 + 1);
     }
     JoinSpace& space = *reinterpret_cast<JoinSpace*>(&s_frag[0][0][0]);
+    __syncthreads();
 #pragma unroll
     for (int side = 0; side < 2; ++side)
-      if (left_w0[side] >= 0) {
-        __syncthreads();   // the LDS of the row before
+      if (s_last[side]) {
         join_row<D>(a, left_w0[side], left_w1[side], left_row[side], left_heads[side], space);
+        __syncthreads();   // its LDS
       }
   }
 
@@ -742,30 +762,85 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
   }
 }
 
+// The rows that several workgroups share, where there are few rows: one row may
+// then be in 256 pieces, too many bytes for one workgroup (a 128K request of one KV
+// head: 36 us with join_row, 24 with this).  A workgroup takes 16 dimensions
+// of a row; its threads take a float4 of a head, of every lots-th piece.
+template <int D>
+__global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs a) {
+  __shared__ float4 s_o[kThreads];
+  __shared__ float2 s_ml[kThreads];
+  const int tid = threadIdx.x;
+  const int item = blockIdx.x / a.per_item, sub = blockIdx.x % a.per_item, x = blockIdx.y;
+  long long start = 0, total = 0;
+  int n = 0;
+  for (int i = 0; i < a.items; ++i) {   // kFewRows at most
+    const int pages = item_pages(a, i);
+    if (i == item) n = pages;
+    if (i < item) start += (long long)pages * a.per_item;
+    total += (long long)pages * a.per_item;
+  }
+  if (n == 0) return;
+  start += (long long)sub * n;
+  const int w0 = share_of(total, start), w1 = share_of(total, start + n - 1);
+  if (w0 == w1) return;
+  int b, g, ht;
+  if (a.l.kv_indptr) b = item / a.G, g = item - b * a.G, ht = sub;
+  else b = item, g = sub / a.HT, ht = sub - g * a.HT;
+  const long long row = (long long)b * a.Hq + g * a.l.group_size + ht * kTileHeads;
+  int heads = a.l.group_size - ht * kTileHeads;
+  heads = heads < kTileHeads ? heads : kTileHeads;
+  const int per = 4 * heads, lots = kThreads / per, lot = tid / per;
+  const int head = (tid - lot * per) >> 2, d = 16 * x + 4 * (tid & 3);
+  float top = -INFINITY, all = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float2 ml, const float4& o) {
+    const float mn = max2(top, ml.x), base = mn == -INFINITY ? 0.f : mn;
+    const float c0 = fast_exp2(top - base), c1 = fast_exp2(ml.x - base);
+    all = all * c0 + ml.y * c1;
+    acc.x = acc.x * c0 + o.x * c1, acc.y = acc.y * c0 + o.y * c1;
+    acc.z = acc.z * c0 + o.z * c1, acc.w = acc.w * c0 + o.w * c1;
+    top = mn;
+  };
+  if (lot < lots)
+#pragma unroll 8
+    for (int e = w0 + lot; e <= w1; e += lots) {
+      const int at = (2 * e + (e == w0 ? 1 : 0)) * kTileHeads + head;
+      add(reinterpret_cast<const float2*>(a.part_ml)[at],
+          *reinterpret_cast<const float4*>(a.part_o + (long long)at * D + d));
+    }
+  // halves: lot i takes lot i + half's
+  for (int n_lots = lots; n_lots > 1;) {
+    const int half = (n_lots + 1) / 2;
+    __syncthreads();
+    if (lot >= half && lot < n_lots) s_o[tid] = acc, s_ml[tid] = make_float2(top, all);
+    __syncthreads();
+    if (lot + half < n_lots) add(s_ml[tid + half * per], s_o[tid + half * per]);
+    n_lots = half;
+  }
+  if (lot > 0) return;
+  const float inv = all == 0.f ? 0.f : 1.f / all;
+  *reinterpret_cast<u32x2*>(a.l.out + (row + head) * D + d) =
+      u32x2{pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)};
+  if (a.l.lse && x == 0 && (tid & 3) == 0)
+    a.l.lse[row + head] = all > 0.f ? (top + __log2f(all)) * kLn2 : -INFINITY;
+}
+
 template <int D, bool VT>
 hipError_t launch(const DecodeArgs& a, hipStream_t st) {
   if (a.l.group_size <= 8) decode_kernel<D, VT, true><<<kGroups, kThreads, 0, st>>>(a);
   else decode_kernel<D, VT, false><<<kGroups, kThreads, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.join_later) return e;
+  decode_join_kernel<D><<<dim3(a.items * a.per_item, D / 16), kThreads, 0, st>>>(a);
   return hipGetLastError();
-}
-
-// A tag per launch: what the workspace held before, an earlier launch's tag among
-// it, does not count as arrived.
-unsigned long long next_tag() {
-  static std::atomic<unsigned long long> next{[] {
-    std::random_device rd;
-    return ((unsigned long long)rd() << 32) ^ rd() ^
-           (unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count();
-  }()};
-  const unsigned long long t = next.fetch_add(1, std::memory_order_relaxed);
-  return t != 0 ? t : next_tag();
 }
 
 }  // namespace
 
 size_t decode_ws_bytes(const CacheDims& d, int) {
   return (size_t)kGroups * (2 * kTileHeads * (d.D * sizeof(float) + sizeof(float2)) +
-                           2 * sizeof(unsigned long long));
+                           sizeof(unsigned long long));
 }
 
 hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& l, hipStream_t st) {
@@ -784,7 +859,8 @@ hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& l, hipStream_t 
   a.part_o = static_cast<float*>(l.ws);
   a.part_ml = a.part_o + (size_t)kGroups * 2 * kTileHeads * d.D;
   a.arrived = reinterpret_cast<unsigned long long*>(a.part_ml + (size_t)kGroups * 2 * kTileHeads * 2);
-  a.tag = next_tag();
+  // a row of at most 32 pieces is joined in the launch, whatever the rows
+  a.join_later = (long long)a.items * a.per_item <= kFewRows && a.max_kv_blocks > 32 * kMinPages;
   const bool vt = d.v_layout != 0;
   if (d.D == 64) return vt ? launch<64, true>(a, st) : launch<64, false>(a, st);
   return vt ? launch<128, true>(a, st) : launch<128, false>(a, st);
