@@ -486,7 +486,7 @@ ca_status ca_release_pages(const ca_cache* c, const int32_t* release, const int3
  *    go to q_out [num_tokens, Hq, D] (dense; q_out may be q if q is dense),
  *    rotated keys and the values to slot_map's places in k_pool and v_pool.
  *    A slot outside [0, num_pages * 64) writes nothing; the slots of one call
- *    must differ from each other.  num_tokens = 0 does nothing.  rot_dim = 0
+ *    must differ from each other.  num_tokens <= 2^23; 0 does nothing.  rot_dim = 0
  *    rotates nothing.  batch and max_kv_blocks of the cache are not used.
  * ---------------------------------------------------------------------- */
 typedef struct ca_rotary {
@@ -517,6 +517,7 @@ ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_to
  *    lse = -inf; a score of NaN or +inf gives out = NaN, lse = -inf, as in
  *    section 3.  A value that is not finite makes the elements of out that it
  *    reaches not finite.  The keys past kv_len may hold anything, NaN included.
+ *    B x max_kv_blocks (with tables: x groups) must be below 2^31.
  *    kv_len is taken as 0 below 0 and as 64 * max_kv_blocks above it; blocks
  *    whose table entry or page id is out of range add no keys.
  *    Workspace: ca_decode_workspace_bytes(c, group_size) bytes, 16-byte aligned,

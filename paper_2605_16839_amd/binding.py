@@ -665,24 +665,28 @@ def assign_slots(c: Cache, new_len: torch.Tensor, num_tokens: int, seq_len: torc
     slots = (T, c.num_kv_heads)
     if "slot_map" not in b:
         b["slot_map"] = torch.empty(slots, dtype=torch.int64, device=new_len.device)
-    sizes = {"positions": T, "token_indptr": B + 1, "granted": B, "seq_len": B, "free_count": 1}
-    missing = [k for k in sizes if k not in b]
+    sizes = (("positions", T), ("token_indptr", B + 1), ("granted", B), ("seq_len", B),
+             ("free_count", 1))
+    missing = [k for k in sizes if k[0] not in b]
+    at = {}
     if missing:   # parts of one tensor: an allocation costs as much as all the checks below
-        n = [sizes[k] for k in missing]
-        parts = torch.empty(sum(n), dtype=i32, device=new_len.device).split_with_sizes(n)
-        b.update(zip(missing, parts))
+        n = [x for _, x in missing]
+        made = torch.empty(sum(n), dtype=i32, device=new_len.device)
+        place = made.data_ptr()
+        for (k, x), part in zip(missing, made.split_with_sizes(n)):
+            b[k], at[k] = part, place
+            place += 4 * x
+    for k, x in sizes:
+        if k not in at:
+            at[k] = _need(k, b[k], i32, (x,), index)
     _check(load().ca_assign_slots(
         c.ref, _need("new_len", new_len, i32, (B,), index), T,
         _need("seq_len", seq_len, i32, (B,), index),
         _need("page_table", page_table, i32, c._table, index),
         _need("free_pages", free_pages, i32, (free_pages.numel(),), index), free_pages.numel(),
         _need("free_count", free_count, i32, (1,), index),
-        _need("slot_map", b["slot_map"], torch.int64, slots, index),
-        _need("positions", b["positions"], i32, (T,), index),
-        _need("token_indptr", b["token_indptr"], i32, (B + 1,), index),
-        _need("granted", b["granted"], i32, (B,), index),
-        _need("seq_len", b["seq_len"], i32, (B,), index),
-        _need("free_count", b["free_count"], i32, (1,), index), st))
+        _need("slot_map", b["slot_map"], torch.int64, slots, index), at["positions"],
+        at["token_indptr"], at["granted"], at["seq_len"], at["free_count"], st))
     return b
 
 

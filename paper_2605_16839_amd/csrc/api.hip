@@ -1003,7 +1003,8 @@ ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_to
   if (r->num_axes < 1 || r->num_axes > 4)
     return fail(CA_ERR_UNSUPPORTED, "num_axes %d not supported (1 to 4)", r->num_axes);
   if (r->rot_dim > 0 && !r->inv_freq) return fail(CA_ERR_NULL, "inv_freq is required");
-  if (num_tokens < 0) return fail(CA_ERR_SHAPE, "num_tokens must be >= 0");
+  if (num_tokens < 0 || num_tokens > 1 << 23)
+    return fail(CA_ERR_SHAPE, "num_tokens %d out of range [0, 2^23]", num_tokens);
   ca::AppendLaunch l = {};
   for (int i = 0; r->pair_axis_host && i < r->rot_dim / 2; ++i) {
     const int axis = r->pair_axis_host[i];

@@ -99,7 +99,7 @@ def test_rotary_refuses(lib, kw, code):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(T=-1), "CA_ERR_SHAPE"), (dict(qs=1016), "CA_ERR_SHAPE"), (dict(ks=248), "CA_ERR_SHAPE"),
+    (dict(T=-1), "CA_ERR_SHAPE"), (dict(T=(1 << 23) + 1), "CA_ERR_SHAPE"), (dict(qs=1016), "CA_ERR_SHAPE"), (dict(ks=248), "CA_ERR_SHAPE"),
     (dict(vs=0), "CA_ERR_SHAPE"), (dict(qs=1028), "CA_ERR_UNALIGNED"), (dict(ks=260), "CA_ERR_UNALIGNED"),
     (dict(q=FAKE + 8), "CA_ERR_UNALIGNED"), (dict(out=FAKE + 8), "CA_ERR_UNALIGNED"),
     (dict(vp=FAKE + 2), "CA_ERR_UNALIGNED"), (dict(slots=FAKE + 4), "CA_ERR_UNALIGNED"),
@@ -129,6 +129,18 @@ def _decode(lib, q=FAKE, kp=FAKE, vp=FAKE, pt=FAKE, kl=FAKE, ip=None, ix=None, g
 ] + [({n: None}, "CA_ERR_NULL") for n in ("q", "kp", "vp", "pt", "kl", "out")])
 def test_decode_attention_refuses(lib, kw, code):
     assert _decode(lib, **kw) == code
+
+
+def test_decode_attention_refuses_rows_past_31_bits(lib):
+    def status(batch, tables, group=0):
+        c = _cache(batch=batch, max_kv_blocks=16384)
+        t = FAKE if tables else None
+        return _name(lib, lib.ca_decode_attention(c.ref, FAKE, FAKE, FAKE, FAKE, FAKE, t, t, group, 0.1,
+                                                  FAKE, None, None, 0, None))
+    assert status(1 << 17, False) == "CA_ERR_SHAPE"
+    assert status((1 << 17) - 1, False) == "CA_ERR_WORKSPACE"       # the next check
+    assert status(1 << 16, True) == "CA_ERR_SHAPE" and status(1 << 15, True, 2) == "CA_ERR_SHAPE"
+    assert status((1 << 16) - 1, True) == "CA_ERR_WORKSPACE"
 
 
 def test_binding_refuses_what_the_kernels_would_misread():
