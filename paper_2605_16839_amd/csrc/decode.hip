@@ -375,6 +375,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
       sub = (int)(off / (unsigned)n);
       sub = sub < a.per_item ? sub : a.per_item - 1;
       p = (int)(off % (unsigned)n);
+    } else {
+      rem = 0;   // as above
     }
   }
   auto part_of = [&](int item, int sub, int n, int p, int left, long long item_start) {
@@ -689,43 +691,45 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
     }
     if (r != at_row) continue;
     at_row += kWaves / per_row;
-    for (int x = wv % per_row; x < NX; x += per_row) {
-      float2 ml[kWaves];
-      float4 o[kWaves];
+    // pieces one after the other, in order, the d tiles of a piece together
+    const int x0 = wv % per_row;
+    float top = -INFINITY, all = 0.f;
+    float4 acc[NX];
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) {   // a wave without a piece: the first piece, not counted
-        const unsigned has = (set >> (2 * v)) & 3;
-        const int at = has ? 2 * v + (int)(has >> 1) : f;
-        ml[v] = s_ml[at >> 1][at & 1][col];
-        o[v] = s_frag[at >> 1][at & 1][64 * x + lane];
+    for (int k = 0; k < NX; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (unsigned rest = set; rest; rest &= rest - 1) {
+      const int at = __builtin_ctz(rest);
+      const float2 ml = s_ml[at >> 1][at & 1][col];
+      const float4* const o = &s_frag[at >> 1][at & 1][64 * x0 + lane];
+      const float mn = max2(top, ml.x), base = mn == -INFINITY ? 0.f : mn;
+      const float c0 = fast_exp2(top - base), c1 = fast_exp2(ml.x - base);
+      all = all * c0 + ml.y * c1;
+      top = mn;
+#pragma unroll
+      for (int k = 0; k < NX; ++k) {
+        if (x0 + k * per_row >= NX) break;
+        const float4 y = o[64 * k * per_row];
+        acc[k].x = acc[k].x * c0 + y.x * c1, acc[k].y = acc[k].y * c0 + y.y * c1;
+        acc[k].z = acc[k].z * c0 + y.z * c1, acc[k].w = acc[k].w * c0 + y.w * c1;
       }
-      float top = ml[0].x;
+    }
+    if (col >= heads) continue;
+    const float inv = all == 0.f ? 0.f : 1.f / all;
 #pragma unroll
-      for (int v = 1; v < kWaves; ++v) top = max2(top, ml[v].x);
-      const float base = top == -INFINITY ? 0.f : top;
-      float all = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
-        const float c = ((set >> (2 * v)) & 3) ? fast_exp2(ml[v].x - base) : 0.f;
-        all += c * ml[v].y;
-        acc.x += c * o[v].x, acc.y += c * o[v].y, acc.z += c * o[v].z, acc.w += c * o[v].w;
-      }
-      if (col < heads) {
-        const int d = 16 * x + 4 * grp;
-        if (flags == 3) {
-          const float inv = all == 0.f ? 0.f : 1.f / all;
-          *reinterpret_cast<u32x2*>(l.out + ((long long)row + col) * D + d) =
-              u32x2{pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv)};
-          if (l.lse && x == 0 && grp == 0)
-            l.lse[row + col] = all > 0.f ? (top + __log2f(all)) * kLn2 : -INFINITY;
-        } else {
-          const int slot = 2 * w + (flags & 1);
-          float* const to = a.part_o + ((long long)slot * kTileHeads + col) * D + d;
-          put2(to, acc.x, acc.y);
-          put2(to + 2, acc.z, acc.w);
-          if (x == 0 && grp == 0) put2(a.part_ml + 2 * (slot * kTileHeads + col), top, all);
-        }
+    for (int k = 0; k < NX; ++k) {
+      const int x = x0 + k * per_row, d = 16 * x + 4 * grp;
+      if (x >= NX) break;
+      if (flags == 3) {
+        *reinterpret_cast<u32x2*>(l.out + ((long long)row + col) * D + d) =
+            u32x2{pack_bf16x2(acc[k].x * inv, acc[k].y * inv), pack_bf16x2(acc[k].z * inv, acc[k].w * inv)};
+        if (l.lse && x == 0 && grp == 0)
+          l.lse[row + col] = all > 0.f ? (top + __log2f(all)) * kLn2 : -INFINITY;
+      } else {
+        const int slot = 2 * w + (flags & 1);
+        float* const to = a.part_o + ((long long)slot * kTileHeads + col) * D + d;
+        put2(to, acc[k].x, acc[k].y);
+        put2(to + 2, acc[k].z, acc[k].w);
+        if (x == 0 && grp == 0) put2(a.part_ml + 2 * (slot * kTileHeads + col), top, all);
       }
     }
   }
