@@ -87,7 +87,7 @@
 extern "C" {
 #endif
 
-#define CA_ABI_VERSION 6
+#define CA_ABI_VERSION 7
 
 typedef enum ca_status {
   CA_OK = 0,

@@ -75,7 +75,7 @@ def _check_assign(B, Hkv, max_blocks, lens, new, table, free, pages, T, in_place
 @pytest.mark.parametrize("B,Hkv,longest,most_new,pad", [
     (1, 1, 0, 1, 0), (1, 8, 700, 2048, 0), (3, 2, 64, 130, 5), (64, 8, 3000, 2, 0),
     (255, 1, 500, 3, 1), (256, 4, 100, 70, 0), (257, 2, 100, 70, 300), (1000, 3, 900, 2, 4),
-    (5, 8, 5000, 3000, 1500),
+    (5, 8, 5000, 3000, 1500), (2, 1500, 70, 70, 3), (2049, 1, 64, 2, 0),
 ])
 def test_assign_slots(B, Hkv, longest, most_new, pad, in_place):
     rng = np.random.default_rng(B * 31 + Hkv)
@@ -331,7 +331,8 @@ def _attention_ok(out, lse, q, kp, vp, table, lens, scale, tables=None, gs=0, he
     assert np.array_equal(np.isfinite(gl), np.isfinite(ref_lse))
     assert (gl[~np.isfinite(ref_lse)] == -np.inf).all()
     fin = np.isfinite(ref_lse)
-    assert (np.abs(gl - ref_lse)[fin] <= (delta[..., 0] + 2.0 ** -20 * np.maximum(1, np.abs(ref_lse)))[fin]).all()
+    d, size = np.abs(gl[fin] - ref_lse[fin]), np.maximum(1, np.abs(ref_lse[fin]))
+    assert (d <= delta[..., 0][fin] + 2.0 ** -20 * size).all()
 
 
 def _run_decode(rng, lens, Hq, Hkv, D, layout, max_blocks=None, gs=0, tables=None, scale=None, qscale=2.0):
@@ -374,6 +375,32 @@ def test_decode_lengths(lens, Hkv, max_blocks):
         _run_decode(rng, lens, 2 * Hkv, Hkv, 64 if len(lens) > 100 else 128, layout, max_blocks)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,lens,max_blocks", [
+    # more than 8 rows: the last workgroup of a row joins it, of many pieces here
+    (4, 1, 128, [20001] + [0] * 8, None), (16, 1, 128, [0] * 9 + [17000], None),
+    (9, 3, 64, [9000, 0, 8191, 1], None), (71, 1, 64, [5000, 70], None),
+    # 8 rows at most and long tables: a launch of its own joins them
+    (4, 1, 128, [30000], 600), (40, 1, 64, [9000], 200), (16, 8, 128, [12000], 2048),
+    (20, 2, 128, [5000, 9001], 300), (1, 1, 64, [16000], 250), (8, 1, 64, [0, 7000, 64], 129),
+])
+def test_decode_rows_of_many_pieces(Hq, Hkv, D, lens, max_blocks):
+    rng = np.random.default_rng(Hq + len(lens))
+    for layout in (0, 1):
+        _run_decode(rng, lens, Hq, Hkv, D, layout, max_blocks)
+
+
+@pytest.mark.parametrize("B", [64, 65, 4096, 4097, 5000])
+def test_decode_many_requests(B):
+    """A lane sums several requests, 64 and more of them at last."""
+    rng = np.random.default_rng(B)
+    lens = np.where(rng.random(B) < 0.7, 0, rng.integers(1, 140, B))
+    lens[[0, B - 1]] = 100, 65
+    _run_decode(rng, lens.tolist(), 2, 1, 64, 0)
+    if B == 4097:
+        _run_decode(rng, [0] * (B - 1) + [1], 2, 1, 64, 0)
+        _run_decode(rng, [300] + [0] * (B - 1), 2, 1, 64, 1)
+
+
 def test_decode_more_rows_than_workgroups():
     rng = np.random.default_rng(0)
     _run_decode(rng, rng.integers(0, 200, 700).tolist(), 8, 8, 64, 0)
@@ -398,6 +425,16 @@ def test_decode_tables(Hq, Hkv, gs, layout):
     tables[3][0] = list(range(79))
     tables[4][-1] = []
     _run_decode(rng, lens, Hq, Hkv, 128, layout, gs=gs, tables=tables)
+
+
+@pytest.mark.parametrize("Hq,Hkv,gs,lens,max_blocks", [(8, 2, 4, [20000], 400), (8, 2, 2, [9000, 0], 200),
+                                                       (40, 1, 20, [9000], 150), (8, 1, 1, [12000], 188)])
+def test_decode_long_tables(Hq, Hkv, gs, lens, max_blocks):
+    rng = np.random.default_rng(gs)
+    tables = [[sorted(rng.choice(-(-n // 64), -(-n // 80), replace=False).tolist()) if n else []
+               for _ in range(Hq // gs)] for n in lens]
+    for layout in (0, 1):
+        _run_decode(rng, lens, Hq, Hkv, 128, layout, max_blocks, gs, tables)
 
 
 def test_decode_out_of_range_is_never_followed():
@@ -662,3 +699,35 @@ def test_another_stream_and_two_workspaces():
     torch.cuda.synchronize()
     for i, x in enumerate(got):
         assert torch.equal(x, want[i % 2])
+
+
+def test_one_workspace_for_several_sizes_and_graphs():
+    """Calls of other sizes, eager and captured, leave a workspace that the next can use."""
+    rng = np.random.default_rng(14)
+    cases = []
+    for lens, Hq, Hkv, D, most in [([7000, 3000], 32, 8, 128, 110), ([500] * 20, 8, 2, 64, 9),
+                                   ([3000, 0, 64], 16, 4, 64, 47), ([12000], 4, 1, 128, 200)]:
+        kp, vp, table, pages = _pools(rng, lens, Hkv, D, most)
+        c = ca.Cache(len(lens), Hq, Hkv, D, most, pages)
+        args = (c, bf16_dev(_bf16(rng, (len(lens), Hq, D))), (bf16_dev(kp), bf16_dev(vp)), i32_dev(table),
+                i32_dev(lens), 0.1)
+        cases.append((args, ca.decode_attention(*args)[0]))
+    ws = torch.full((max(ca.decode_workspace_bytes(a[0]) for a, _ in cases),), 0xff, dtype=torch.uint8, device=DEV)
+    for _ in range(3):
+        for args, want in cases:
+            assert torch.equal(ca.decode_attention(*args, ws=ws)[0], want)
+    torch.cuda.synchronize()
+    graphs = []
+    for args, want in cases[:2]:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out, _ = ca.decode_attention(*args, ws=ws)
+        graphs.append((g, out, want))
+    for i in range(4):
+        for g, out, want in graphs:
+            out.zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want), i
+        args, want = cases[2 + i % 2]
+        assert torch.equal(ca.decode_attention(*args, ws=ws)[0], want)
