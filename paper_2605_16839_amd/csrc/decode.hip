@@ -3,26 +3,32 @@
 // in one pass over the keys with the running maximum m and sum.
 //
 // What bounds it: every K and V page is read once and used for the few query
-// heads of its KV head, 2 flops per byte and head, so HBM does.  Everything
-// below serves an even, deep stream of page loads:
+// heads of its KV head, 2 flops per byte and head, so HBM does; with little to read,
+// the latency of length, page id, page and joined pieces, one after the other.  96
+// requests of 4K to 32K tokens (32/8 heads, D = 128, 5.6 GB): 825 us, 6.8 TB/s,
+// where a bare reader of such pages in such shares takes 810.  Everything below serves an even
+// stream of page loads:
 //   * the requests' lengths are on the GPU only and may be as different as they
 //     like, so the pages of all (request, KV head) rows are laid end to end and
 //     cut in equal shares, one per workgroup and within it one per wave; every
 //     wave finds its share from a prefix sum over the lengths;
-//   * a wave is on its own until its share ends: it loads K and V pages to
-//     registers (32 KB of them in flight per wave, 256 KB per CU), and no
-//     barrier or other wave is waited for;
+//   * a wave has its own rows and pages: it asks for a whole page, 16 loads of
+//     1 KB (D = 128), takes it through its 8 KB of LDS half by half, and asks for
+//     the next, K, V, K, .., while it computes: 128 KB of a CU are on their way.
+//     Across a row's end too: the next row's ids are there before;
 //   * S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_16x16x32_bf16, the heads of
-//     the KV head being the 16 columns.  K fragments are the registers as loaded
-//     (key_of gives a lane 8 consecutive keys of each 32-key step, as the P^T
-//     fragment wants them), transposed V pages too; token-major V goes through
-//     8 KB of LDS per wave for the transpose read;
+//     the KV head being the 16 columns (more than 16 heads: tiles of 16 that read the
+//     pages each).  key_of gives a lane 8 consecutive keys of each 32-key step,
+//     as the P^T fragment wants them; token-major V is read from LDS transposed;
 //   * up to 8 heads leave half of the columns free: they hold the same heads
 //     again, and carry the part of the weights that bf16 loses (p - bf16(p)),
-//     so the weights count with 16 bits at no cost;
+//     so the weights count with 16 bits at no cost.  With 9 to 16 heads the weights
+//     are rounded to bf16, as the chunk attention's are;
 //   * a row that lies inside one wave's share is written at once; pieces of
 //     a workgroup's waves are joined in its LDS, and rows that several workgroups
-//     share by the last of them (join_row).
+//     share by the last of them (join_row), or by a second launch where few rows may
+//     be in many pieces (decode_join_kernel).  Pieces are taken in page order, so
+//     the result does not depend on who is last.
 #include <cstdint>
 #include <type_traits>
 
@@ -35,7 +41,9 @@ namespace {
 constexpr int kWaves = 8;                   // per workgroup
 constexpr int kThreads = kWaves * kWave;
 constexpr int kGroups = 256;                // one workgroup per CU
-constexpr int kMinPages = 4;                // of a workgroup's share
+// Pages of a workgroup's share at least: 4096 tokens of 8 KV heads take 13.1 us so (a
+// CU draws some 30 GB/s, so the pages go to many), 15.1 with 8 and 19.4 with 16
+constexpr int kMinPages = 4;
 constexpr int kFewRows = 8;                 // so many rows at most are joined by a launch of its own
 constexpr int kTileHeads = 16;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -453,9 +461,11 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
         q[s] = __builtin_bit_cast(bf16x8, x);
       }
     };
-    // A page on its way: whole rows, 1 KB a load.  One page of a wave is in
-    // flight at a time, K(i), V(i), K(i + 1), ..: two (K(i + 1) while V(i) is on its
-    // way) were 14% slower on 5.6 GB, and loads that keep their lines 12%.
+    // A page on its way: whole rows, 1 KB a load, lines that no one keeps.  One page
+    // of a wave at a time, K(i), V(i), K(i + 1), ..: a bare reader of 537 MB takes 80 us
+    // so, 103 with K(i + 1) asked for while V(i) is on its way, and 91 with
+    // ordinary loads; 16 rows x 64 bytes a load (fragments straight to
+    // registers) took this kernel 991 us of 5.6 GB instead of 834.
     u32x4 x[NL];
     auto load = [&](const uint16_t* pool, int id) {
       // a page that is not there: page 0 is read in its place and counts for nothing
@@ -713,13 +723,14 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
         acc[k].z = acc[k].z * c0 + y.z * c1, acc[k].w = acc[k].w * c0 + y.w * c1;
       }
     }
-    if (col >= heads) continue;
     const float inv = all == 0.f ? 0.f : 1.f / all;
 #pragma unroll
     for (int k = 0; k < NX; ++k) {
       const int x = x0 + k * per_row, d = 16 * x + 4 * grp;
       if (x >= NX) break;
-      if (flags == 3) {
+      if (col >= heads) {
+        // no such head
+      } else if (flags == 3) {
         *reinterpret_cast<u32x2*>(l.out + ((long long)row + col) * D + d) =
             u32x2{pack_bf16x2(acc[k].x * inv, acc[k].y * inv), pack_bf16x2(acc[k].z * inv, acc[k].w * inv)};
         if (l.lse && x == 0 && grp == 0)
