@@ -60,7 +60,8 @@ def _check_assign(B, Hkv, max_blocks, lens, new, table, free, pages, T, in_place
     c = ca.Cache(B, Hkv, Hkv, 64, max_blocks, pages)
     seq, count, pt = i32_dev(lens), i32_dev([len(free)]), i32_dev(table)
     fp = _free_dev(free, capacity or len(free) + 1)
-    bufs = dict(seq_len=seq, free_count=count) if in_place else {}
+    bufs = {True: dict(seq_len=seq, free_count=count), "len": dict(seq_len=seq),
+            "count": dict(free_count=count)}.get(in_place, {})
     got = ca.assign_slots(c, i32_dev(new), T, seq, pt, fp, count, bufs)
     torch.cuda.synchronize()
     for key in ("slot_map", "positions", "token_indptr", "granted", "seq_len", "free_count"):
@@ -71,7 +72,7 @@ def _check_assign(B, Hkv, max_blocks, lens, new, table, free, pages, T, in_place
         assert np.array_equal(seq.cpu().numpy(), lens) and int(count) == len(free)
 
 
-@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("in_place", [False, True, "len", "count"])
 @pytest.mark.parametrize("B,Hkv,longest,most_new,pad", [
     (1, 1, 0, 1, 0), (1, 8, 700, 2048, 0), (3, 2, 64, 130, 5), (64, 8, 3000, 2, 0),
     (255, 1, 500, 3, 1), (256, 4, 100, 70, 0), (257, 2, 100, 70, 300), (1000, 3, 900, 2, 4),
@@ -86,7 +87,7 @@ def test_assign_slots(B, Hkv, longest, most_new, pad, in_place):
 
 
 @pytest.mark.parametrize("case", ["no_tokens", "no_pages", "few_pages", "rows_end", "too_long",
-                                  "bad_lengths", "bad_pages", "huge_new", "no_list"])
+                                  "bad_lengths", "bad_pages", "bad_free_pages", "huge_new", "no_list"])
 def test_assign_slots_bounds(case):
     rng = np.random.default_rng(5)
     B, Hkv, max_blocks = 300, 2, 6
@@ -113,6 +114,8 @@ def test_assign_slots_bounds(case):
         table[10:60] = pages
         table[60:90] = -2**31
         lens[10:90] |= 1      # their last block is held
+    elif case == "bad_free_pages":    # they are given away, but nothing is written to them
+        free[-40::3] = [pages, -1, -2**31, 2**31 - 1] * 3 + [pages + 1] * 2
     elif case == "huge_new":
         new[100:] = 2**31 - 1   # the row sum passes 32 bits
     elif case == "no_list":
@@ -679,6 +682,33 @@ def test_captured_step_replays_while_requests_grow():
         assert torch.equal(out, eout) and torch.equal(lse[id(a)], lse[id(e)])
         assert torch.equal(a.state["seq_len"], e.state["seq_len"])
         assert torch.equal(a.table, e.table) and torch.equal(a.pools[0], e.pools[0])
+
+
+def test_streams_by_argument():
+    """stream= takes each call to that stream: after work there that the current stream lacks."""
+    rng = np.random.default_rng(15)
+    B, Hq, Hkv, D, most, pages = 3, 4, 2, 64, 4, 30
+    a, e = (_Server(np.random.default_rng(2), B, Hq, Hkv, D, most, pages, 0) for _ in range(2))
+    qkv, new = bf16_dev(_bf16(rng, (B, Hq + 2 * Hkv, D))), i32_dev([1, 1, 1])
+    eb, eq = e.step(new, qkv, B)
+    eout, _ = ca.decode_attention(e.c, eq, e.pools, e.table, e.state["seq_len"], e.scale)
+    elen, ecount = ca.release_pages(e.c, i32_dev([0, 1, 0]), e.state["seq_len"], e.table, e.free, e.state["free_count"])
+    st = torch.cuda.Stream()
+    late, q, out = torch.zeros_like(qkv), torch.empty(B, Hq, D, dtype=qkv.dtype, device=DEV), torch.empty_like(eout)
+    bufs = {**{k: torch.zeros_like(v) for k, v in eb.items()}, **a.state}
+    flags, ended = i32_dev([0, 1, 0]), (torch.empty_like(elen), torch.empty_like(ecount))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        torch.cuda._sleep(20_000_000)
+        late.copy_(qkv)
+    ca.assign_slots(a.c, new, B, a.state["seq_len"], a.table, a.free, a.state["free_count"], bufs, stream=st)
+    ca.rotary_append(a.c, a.rot, late[:, :Hq], late[:, Hq:Hq + Hkv], late[:, Hq + Hkv:], bufs["positions"],
+                     bufs["slot_map"], a.pools, out=q, stream=st)
+    ca.decode_attention(a.c, q, a.pools, a.table, a.state["seq_len"], a.scale, out=out, ws=a.ws, stream=st)
+    ca.release_pages(a.c, flags, a.state["seq_len"], a.table, a.free, a.state["free_count"], out=ended, stream=st)
+    st.synchronize()
+    assert torch.equal(q, eq) and torch.equal(out, eout) and torch.equal(a.pools[0], e.pools[0])
+    assert torch.equal(ended[0], elen) and torch.equal(ended[1], ecount) and torch.equal(a.free, e.free)
 
 
 def test_another_stream_and_two_workspaces():
