@@ -756,10 +756,11 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
     }
     JoinSpace& space = *reinterpret_cast<JoinSpace*>(&s_frag[0][0][0]);
     __syncthreads();
-#pragma unroll
-    for (int side = 0; side < 2; ++side)
+#pragma nounroll
+    for (int side = 0; side < 2; ++side)   // one copy of the code: it is cold when it is needed
       if (s_last[side]) {
-        join_row<D>(a, left_w0[side], left_w1[side], left_row[side], left_heads[side], space);
+        join_row<D>(a, side ? left_w0[1] : left_w0[0], side ? left_w1[1] : left_w1[0],
+                    side ? left_row[1] : left_row[0], side ? left_heads[1] : left_heads[0], space);
         __syncthreads();   // its LDS
       }
   }
