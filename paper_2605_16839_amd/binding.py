@@ -661,17 +661,18 @@ def assign_slots(c: Cache, new_len: torch.Tensor, num_tokens: int, seq_len: torc
     free_count [1] after the step; the last two may be the inputs themselves."""
     index, st = _here(new_len, stream)
     i32, B, T = torch.int32, c.batch, num_tokens
+    new = _need("new_len", new_len, i32, (B,), index)
     b = bufs if bufs is not None else {}
     slots = (T, c.num_kv_heads)
     if "slot_map" not in b:
-        b["slot_map"] = torch.empty(slots, dtype=torch.int64, device=new_len.device)
+        b["slot_map"] = new_len.new_empty(slots, dtype=torch.int64)
     sizes = (("positions", T), ("token_indptr", B + 1), ("granted", B), ("seq_len", B),
              ("free_count", 1))
     missing = [k for k in sizes if k[0] not in b]
     at = {}
     if missing:   # parts of one tensor: an allocation costs as much as all the checks below
         n = [x for _, x in missing]
-        made = torch.empty(sum(n), dtype=i32, device=new_len.device)
+        made = new_len.new_empty(sum(n))
         place = made.data_ptr()
         for (k, x), part in zip(missing, made.split_with_sizes(n)):
             b[k], at[k] = part, place
@@ -680,7 +681,7 @@ def assign_slots(c: Cache, new_len: torch.Tensor, num_tokens: int, seq_len: torc
         if k not in at:
             at[k] = _need(k, b[k], i32, (x,), index)
     _check(load().ca_assign_slots(
-        c.ref, _need("new_len", new_len, i32, (B,), index), T,
+        c.ref, new, T,
         _need("seq_len", seq_len, i32, (B,), index),
         _need("page_table", page_table, i32, c._table, index),
         _need("free_pages", free_pages, i32, (free_pages.numel(),), index), free_pages.numel(),
@@ -697,14 +698,14 @@ def release_pages(c: Cache, release: torch.Tensor, seq_len: torch.Tensor,
     Returns (seq_len, free_count) after it, which may be the inputs themselves (``out``)."""
     index, st = _here(release, stream)
     i32, B = torch.int32, c.batch
+    lens, count = _need("seq_len", seq_len, i32, (B,), index), _need("free_count", free_count, i32, (1,), index)
     if out is None:
-        out = torch.empty(B + 1, dtype=i32, device=release.device).split_with_sizes((B, 1))
+        out = (torch.empty_like(seq_len), torch.empty_like(free_count))
     _check(load().ca_release_pages(
-        c.ref, _need("release", release, i32, (B,), index),
-        _need("seq_len", seq_len, i32, (B,), index),
+        c.ref, _need("release", release, i32, (B,), index), lens,
         _need("page_table", page_table, i32, c._table, index),
         _need("free_pages", free_pages, i32, (free_pages.numel(),), index), free_pages.numel(),
-        _need("free_count", free_count, i32, (1,), index), _need("seq_len", out[0], i32, (B,), index),
+        count, _need("seq_len", out[0], i32, (B,), index),
         _need("free_count", out[1], i32, (1,), index), st))
     return out
 
@@ -731,9 +732,9 @@ def rotary_append(c: Cache, r: Rotary, q: torch.Tensor, k: torch.Tensor, v: torc
     index, st = _here(q, stream)
     bf = torch.bfloat16
     T, Hq, Hkv, D = q.shape[0], c.num_q_heads, c.num_kv_heads, c.head_dim
-    if out is None:
-        out = torch.empty((T, Hq, D), dtype=bf, device=q.device)
     qp, qs = _rows("q", q, (T, Hq, D), index)
+    if out is None:   # dense: q's tokens are, or lie apart
+        out = torch.empty_like(q)
     kp, ks = _rows("k", k, (T, Hkv, D), index)
     vp, vs = _rows("v", v, (T, Hkv, D), index)
     place = (T,) if r.num_axes == 1 and positions.dim() == 1 else (r.num_axes, T)
@@ -765,8 +766,9 @@ def decode_attention(c: Cache, q: torch.Tensor, kv_pool: Tuple[torch.Tensor, tor
     index, st = _here(q, stream)
     bf, i32 = torch.bfloat16, torch.int32
     shape = (c.batch, c.num_q_heads, c.head_dim)
+    qp = _need("q", q, bf, shape, index)
     if out is None:
-        out = torch.empty(shape, dtype=bf, device=q.device)
+        out = torch.empty_like(q)
     if ws is None:
         n = decode_workspace_bytes(c, group_size)
         ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
@@ -779,7 +781,7 @@ def decode_attention(c: Cache, q: torch.Tensor, kv_pool: Tuple[torch.Tensor, tor
         indptr = _need("kv_indptr", tables[0], i32, (rows + 1,), index)
         indices = _need("kv_indices", tables[1], i32, (rows * c.max_kv_blocks,), index)
     _check(load().ca_decode_attention(
-        c.ref, _need("q", q, bf, shape, index), _need("k_pool", kv_pool[0], bf, c._k_pool, index),
+        c.ref, qp, _need("k_pool", kv_pool[0], bf, c._k_pool, index),
         _need("v_pool", kv_pool[1], bf, c._v_pool, index),
         _need("page_table", page_table, i32, c._table, index),
         _need("kv_len", kv_len, i32, (c.batch,), index), indptr, indices, group_size, sm_scale,
