@@ -452,8 +452,8 @@ ca_status ca_check_cache(const ca_cache* c, int32_t group_size);
  *    requests after the first that do not fit as well, if they hold any.
  *
  *    seq_len_out may be seq_len and free_count_out may be free_count (the step
- *    is then in place, and one workgroup does it all, which is enough for
- *    decode steps); no other buffers may overlap.  num_tokens may be 0.
+ *    is then in place; more than a decode step's rows then take two launches);
+ *    no other buffers may overlap.  num_tokens may be 0.
  * ---------------------------------------------------------------------- */
 ca_status ca_assign_slots(const ca_cache* c, const int32_t* new_len, int32_t num_tokens,
                           const int32_t* seq_len, int32_t* page_table,

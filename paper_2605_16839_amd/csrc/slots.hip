@@ -20,7 +20,8 @@ namespace {
 constexpr int kSlotThreads = 1024;
 constexpr int kSlotWaves = kSlotThreads / kWave;
 constexpr int kSlotGroups = 256;
-constexpr int kReleaseGroups = 16;
+constexpr int kReleaseGroups = 64;
+constexpr int kAloneRounds = 4;   // of one workgroup's threads, where it works alone
 
 // The value of a lane before this one in 64-bit halves (0 where there is none).
 template <int CTRL, int ROWS>
@@ -87,7 +88,10 @@ struct SlotArgs {
   int B, Hkv, max_kv_blocks, num_pages;
   int rows_at_once;   // token rows that a workgroup's threads write together
   int rows_per_wg;    // a multiple of it
+  int what;           // kRows, kState: what this launch writes
 };
+constexpr int kRows = 1;    // token rows and page-table entries, or the free list
+constexpr int kState = 2;   // everything by request
 
 __global__ __launch_bounds__(kSlotThreads) void assign_slots_kernel(const SlotArgs a) {
   __shared__ Sums s_part[kSlotWaves];
@@ -97,10 +101,10 @@ __global__ __launch_bounds__(kSlotThreads) void assign_slots_kernel(const SlotAr
   __shared__ long long s_given;
   const SlotLaunch& l = a.l;
   const int tid = threadIdx.x, H = a.Hkv;
-  const bool first = blockIdx.x == 0;
+  const bool first = blockIdx.x == 0 && (a.what & kState);
   const long long T = l.num_tokens;
   long long lo = (long long)blockIdx.x * a.rows_per_wg;
-  long long hi = lo + a.rows_per_wg;
+  long long hi = a.what & kRows ? lo + a.rows_per_wg : lo;
   lo = lo < T ? lo : T;
   hi = hi < T ? hi : T;
   // this thread's row among those written together, and its first head
@@ -183,7 +187,7 @@ __global__ __launch_bounds__(kSlotThreads) void release_pages_kernel(const SlotA
   __shared__ long long s_given;
   const SlotLaunch& l = a.l;
   const int tid = threadIdx.x, H = a.Hkv;
-  const bool first = blockIdx.x == 0;
+  const bool first = blockIdx.x == 0 && (a.what & kState);
   int count = l.free_count[0];
   count = count < 0 ? 0 : (count > l.free_capacity ? l.free_capacity : count);
   if (tid == 0) s_given = 0;
@@ -207,8 +211,8 @@ __global__ __launch_bounds__(kSlotThreads) void release_pages_kernel(const SlotA
     }
     __syncthreads();
     const int n_here = a.B - b0 < kSlotThreads ? a.B - b0 : kSlotThreads;
-    const long long end = sum0 + all.a;
-    for (long long x = sum0 + (long long)blockIdx.x * kSlotThreads + tid; x < end;
+    const long long end = sum0 + all.a, stop = a.what & kRows ? end : sum0;
+    for (long long x = sum0 + (long long)blockIdx.x * kSlotThreads + tid; x < stop;
          x += (long long)gridDim.x * kSlotThreads) {
       const int i = last_at_most(s_start, n_here, x);
       if (s_kept[i]) continue;
@@ -223,27 +227,44 @@ __global__ __launch_bounds__(kSlotThreads) void release_pages_kernel(const SlotA
 
 }  // namespace
 
-// In place, one workgroup does it all: it reads a length before it writes it, and
-// no other workgroup reads it.  Else as many as write their rows in one go
-// (8256 rows of 8 heads: 218 us with one, 5.3 with 65).
+// As many workgroups as write their rows in one go (8256 rows of 8 heads: 71 us with
+// one, 4.7 with 65).  In place, no workgroup may write a length that another has yet
+// to read: one does it all where it has little to write (256 rows of 8 heads: 5.4
+// us, and 4.8 out of place), else a second launch writes what is known by request.
 hipError_t launch_assign_slots(const CacheDims& d, const SlotLaunch& l, hipStream_t st) {
-  SlotArgs a{l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, 0, 0};
+  SlotArgs a{l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, 0, 0, kRows | kState};
   a.rows_at_once = d.Hkv < kSlotThreads ? kSlotThreads / d.Hkv : 1;
   const bool in_place = l.seq_len_out == l.seq_len || l.free_count_out == l.free_count;
   const long long rounds = ((long long)l.num_tokens + a.rows_at_once - 1) / a.rows_at_once;
+  const bool alone = in_place && rounds <= kAloneRounds;
   // at most kSlotGroups, so that few workgroups repeat the sums
-  const long long each = in_place ? rounds : (rounds + kSlotGroups - 1) / kSlotGroups;
+  const long long each = alone ? rounds : (rounds + kSlotGroups - 1) / kSlotGroups;
   const long long per_wg = (each > 0 ? each : 1) * a.rows_at_once;
   a.rows_per_wg = (int)(per_wg < INT32_MAX ? per_wg : INT32_MAX);
-  const int grid = in_place || rounds == 0 ? 1 : (int)((rounds + each - 1) / each);
+  const int grid = alone || rounds == 0 ? 1 : (int)((rounds + each - 1) / each);
+  if (in_place && !alone) a.what = kRows;
   assign_slots_kernel<<<grid, kSlotThreads, 0, st>>>(a);
+  if (a.what != kRows) return hipGetLastError();
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  a.what = kState;
+  assign_slots_kernel<<<1, kSlotThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
+// 64 requests of 512 blocks and 8 heads: 213 us with one workgroup, 17.9 with 16, 8.0
+// with 64; 9 of 256 requests of 40 blocks: 5.6, 3.8 and 3.8.  In place as above.
 hipError_t launch_release_pages(const CacheDims& d, const SlotLaunch& l, hipStream_t st) {
-  SlotArgs a{l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, 0, 0};
+  SlotArgs a{l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, 0, 0, kRows | kState};
   const bool in_place = l.seq_len_out == l.seq_len || l.free_count_out == l.free_count;
-  release_pages_kernel<<<in_place ? 1 : kReleaseGroups, kSlotThreads, 0, st>>>(a);
+  const bool alone = (long long)d.B * d.Hkv * d.max_kv_blocks <= kAloneRounds * kSlotThreads;
+  if (in_place && !alone) a.what = kRows;
+  release_pages_kernel<<<alone ? 1 : kReleaseGroups, kSlotThreads, 0, st>>>(a);
+  if (a.what != kRows) return hipGetLastError();
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  a.what = kState;
+  release_pages_kernel<<<1, kSlotThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 

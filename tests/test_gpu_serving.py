@@ -748,7 +748,7 @@ def test_one_workspace_for_several_sizes_and_graphs():
             assert torch.equal(ca.decode_attention(*args, ws=ws)[0], want)
     torch.cuda.synchronize()
     graphs = []
-    for args, want in cases[:2]:
+    for args, want in (cases[0], cases[1], cases[3]):
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
             out, _ = ca.decode_attention(*args, ws=ws)
