@@ -41,10 +41,9 @@ namespace {
 constexpr int kWaves = 8;                   // per workgroup
 constexpr int kThreads = kWaves * kWave;
 constexpr int kGroups = 256;                // one workgroup per CU
-// Pages of a workgroup's share at least: 4096 tokens of 8 KV heads take 13.1 us so (a
-// CU draws some 30 GB/s, so the pages go to many), 15.1 with 8 and 19.4 with 16
-constexpr int kMinPages = 4;
 constexpr int kFewRows = 8;                 // so many rows at most are joined by a launch of its own
+constexpr int kManyPieces = 64;             // .. and if a row may have more than so many pages
+constexpr int kShortRow = 4;                // pages
 constexpr int kTileHeads = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -99,18 +98,33 @@ __device__ __forceinline__ float other_half(float x) {
 // 2^x, and the maxima in log2 units: exp2 of -inf is 0.
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Pages of a workgroup's share at least.  A CU draws some 30 GB/s, so few pages go to
+// many: 2 to each for 1024 tokens of 8 KV heads take 10.2 us, 4 take 11.8 and 8 14.5 (1
+// takes 9.8, but 16K tokens of one KV head then 16.1 instead of 12.4: pieces to join).
+// One page each where 128 or fewer are there: 700 tokens of one KV head take 8.4 us, 9.0
+// with two.  Rows of up to kShortRow pages on average stay whole, as a join costs
+// more than their other pages: 128 tokens of 8 KV heads take 7.9 us so, 9.7 with a page
+// each; rows of 8 pages take 11.1 whole, 9.8 cut.
+__device__ __forceinline__ int least_pages(const DecodeArgs& a, long long total) {
+  if (total >= kGroups * kShortRow) return 1;   // every share has more
+  const int pages = (int)total;
+  const long long rows = (long long)a.items * a.per_item;
+  if (pages <= rows) return 1;
+  if (pages <= rows * kShortRow) return (pages + (int)rows - 1) / (int)rows;
+  return pages <= kGroups / 2 ? 1 : 2;
+}
 // First page of share w when `total` pages are dealt, and the share of page u.
-__device__ __forceinline__ long long share_start(long long total, int w) {
-  if (total >= (long long)kGroups * kMinPages) return (total * w) / kGroups;
-  const long long s = (long long)w * kMinPages;
+__device__ __forceinline__ long long share_start(long long total, int least, int w) {
+  if (total >= (long long)kGroups * least) return (total * w) / kGroups;
+  const long long s = (long long)w * least;
   return s < total ? s : total;
 }
-__device__ __forceinline__ int share_of(long long total, long long u) {
-  if (total < (long long)kGroups * kMinPages) return (int)u / kMinPages;
+__device__ __forceinline__ int share_of(long long total, int least, long long u) {
+  if (total < (long long)kGroups * least) return (int)u / least;
   int w = (int)((float)u / (float)total * kGroups);   // off by one at most
   w = w < kGroups - 1 ? w : kGroups - 1;
-  if (share_start(total, w) > u) return w - 1;
-  return share_start(total, w + 1) <= u ? w + 1 : w;
+  if (share_start(total, least, w) > u) return w - 1;
+  return share_start(total, least, w + 1) <= u ? w + 1 : w;
 }
 
 // Sum over the lanes up to this one.
@@ -341,7 +355,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
   auto pages_of = [&](int i) -> int {
     return per == 1 ? __builtin_amdgcn_readlane((int)mine, i) : uniform(item_pages(a, i));
   };
-  const long long u0 = share_start(total, w), nu = share_start(total, w + 1) - u0;
+  const int least = least_pages(a, total);
+  const long long u0 = share_start(total, least, w), nu = share_start(total, least, w + 1) - u0;
   const long long my0 = u0 + nu * wv / kWaves, my1 = u0 + nu * (wv + 1) / kWaves;
   if (lane < 2) s_meta[wv][lane].z = 0;
 
@@ -694,8 +709,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
     const int row = __builtin_amdgcn_readlane(meta.x, f), heads = __builtin_amdgcn_readlane(meta.y, f);
     if (flags != 3) {
       const int side = flags & 1;
-      const int w0 = share_of(total, uniform64(s_row[f >> 1][f & 1][0]));
-      const int w1 = share_of(total, uniform64(s_row[f >> 1][f & 1][1]));
+      const int w0 = share_of(total, least, uniform64(s_row[f >> 1][f & 1][0]));
+      const int w1 = share_of(total, least, uniform64(s_row[f >> 1][f & 1][1]));
       if (side) left_w0[1] = w0, left_w1[1] = w1, left_heads[1] = heads, left_row[1] = row;
       else left_w0[0] = w0, left_w1[0] = w1, left_heads[0] = heads, left_row[0] = row;
     }
@@ -798,7 +813,8 @@ __global__ __launch_bounds__(kThreads) void decode_join_kernel(const DecodeArgs 
   }
   if (n == 0) return;
   start += (long long)sub * n;
-  const int w0 = share_of(total, start), w1 = share_of(total, start + n - 1);
+  const int least = least_pages(a, total);
+  const int w0 = share_of(total, least, start), w1 = share_of(total, least, start + n - 1);
   if (w0 == w1) return;
   int b, g, ht;
   if (a.l.kv_indptr) b = item / a.G, g = item - b * a.G, ht = sub;
@@ -875,8 +891,8 @@ hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& l, hipStream_t 
   a.part_o = static_cast<float*>(l.ws);
   a.part_ml = a.part_o + (size_t)kGroups * 2 * kTileHeads * d.D;
   a.arrived = reinterpret_cast<unsigned long long*>(a.part_ml + (size_t)kGroups * 2 * kTileHeads * 2);
-  // a row of at most 32 pieces is joined in the launch, whatever the rows
-  a.join_later = (long long)a.items * a.per_item <= kFewRows && a.max_kv_blocks > 32 * kMinPages;
+  // a row of at most 64 pieces (32 and fewer as a rule) is joined in the launch, whatever the rows
+  a.join_later = (long long)a.items * a.per_item <= kFewRows && a.max_kv_blocks > kManyPieces;
   const bool vt = d.v_layout != 0;
   if (d.D == 64) return vt ? launch<64, true>(a, st) : launch<64, false>(a, st);
   return vt ? launch<128, true>(a, st) : launch<128, false>(a, st);

@@ -392,6 +392,20 @@ def test_decode_rows_of_many_pieces(Hq, Hkv, D, lens, max_blocks):
         _run_decode(rng, lens, Hq, Hkv, D, layout, max_blocks)
 
 
+@pytest.mark.parametrize("lens,Hkv,max_blocks", [
+    # on both sides of a page to a workgroup (128 pages), of two (512), of whole rows (4 pages on average)
+    ([64 * 64], 1, 64), ([64 * 128], 1, 129), ([64 * 128 + 1], 1, 129), ([64 * 64], 2, 64),
+    ([64 * 511 + 9], 1, 512), ([64 * 512], 1, 512), ([64 * 513], 1, 513),
+    ([256], 8, 4), ([257], 8, 5), ([192, 130, 1], 8, None), ([900, 1, 1, 60], 2, None),
+    ([300, 1, 64, 0, 190, 256, 512, 1], 16, None), ([256] * 32, 8, None), ([256] * 31 + [257], 8, None),
+    ([3000] + [64] * 60, 4, None), ([64] * 255 + [4000], 1, None),
+])
+def test_decode_few_pages(lens, Hkv, max_blocks):
+    rng = np.random.default_rng(sum(lens) + Hkv)
+    for layout in (0, 1):
+        _run_decode(rng, lens, 4 * Hkv, Hkv, 64, layout, max_blocks)
+
+
 @pytest.mark.parametrize("B", [64, 65, 4096, 4097, 5000])
 def test_decode_many_requests(B):
     """A lane sums several requests, 64 and more of them at last."""
