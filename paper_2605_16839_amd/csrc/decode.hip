@@ -113,18 +113,24 @@ __device__ __forceinline__ int least_pages(const DecodeArgs& a, long long total)
   if (pages <= rows * kShortRow) return (pages + (int)rows - 1) / (int)rows;
   return pages <= kGroups / 2 ? 1 : 2;
 }
+
 // First page of share w when `total` pages are dealt, and the share of page u.
 __device__ __forceinline__ long long share_start(long long total, int least, int w) {
   if (total >= (long long)kGroups * least) return (total * w) / kGroups;
   const long long s = (long long)w * least;
   return s < total ? s : total;
 }
+// Below kGroups also for a page that is none of `total` (lengths changed under the kernel).
 __device__ __forceinline__ int share_of(long long total, int least, long long u) {
-  if (total < (long long)kGroups * least) return (int)u / least;
-  int w = (int)((float)u / (float)total * kGroups);   // off by one at most
-  w = w < kGroups - 1 ? w : kGroups - 1;
-  if (share_start(total, least, w) > u) return w - 1;
-  return share_start(total, least, w + 1) <= u ? w + 1 : w;
+  int w;
+  if (total < (long long)kGroups * least) {
+    w = (int)u / least;
+  } else {
+    w = (int)((float)u / (float)total * kGroups);   // off by one at most
+    if (w > 0 && share_start(total, least, w) > u) --w;
+    else if (share_start(total, least, w + 1) <= u) ++w;
+  }
+  return w < 0 ? 0 : (w < kGroups - 1 ? w : kGroups - 1);
 }
 
 // Sum over the lanes up to this one.
