@@ -508,7 +508,11 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
       __builtin_amdgcn_wave_barrier();
     };
     f32x4 o[NX];
-    float m, sum;   // m: of q.k, before the scale
+    // m is carried scaled and rounded, as the weights take it off: while the maximum
+    // stays, its factor is 1 exactly.  Scaled anew for every page it would be fused into the
+    // difference and leave the product's rounding there, on all earlier pages, every time
+    // (512 pages to a wave, largest scores of 180 in each: lse 2.6e-3 off, 5e-6 so).
+    float m, sum;
     auto clear = [&] {
 #pragma unroll
       for (int x = 0; x < NX; ++x) o[x] = {0.f, 0.f, 0.f, 0.f};
@@ -562,9 +566,9 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = max2(top, s[t][e]);
-      const float mn = max2(m, groups_max(top));
-      const float base = mn == -INFINITY ? 0.f : mn * a.scale_log2;
-      const float alpha = fast_exp2(m * a.scale_log2 - base);
+      const float mn = max2(m, groups_max(top) * a.scale_log2);
+      const float base = mn == -INFINITY ? 0.f : mn;
+      const float alpha = fast_exp2(m - base);
       m = mn;
       float part = 0.f;
 #pragma unroll
@@ -652,7 +656,6 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
         for (int x = 0; x < NX; ++x)
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[x][e] += other_half(o[x][e]);
-      const float ml = m * a.scale_log2;
       const bool starts = cur.p == 0, ends = cur.p + cur.cnt == cur.n;
       if (starts && ends) {
         if (col < cur.heads) {
@@ -662,14 +665,14 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
           for (int x = 0; x < NX; ++x)
             *reinterpret_cast<u32x2*>(l.out + row * D + 16 * x + 4 * grp) =
                 u32x2{pack_bf16x2(o[x][0] * inv, o[x][1] * inv), pack_bf16x2(o[x][2] * inv, o[x][3] * inv)};
-          if (l.lse && grp == 0) l.lse[row] = sum > 0.f ? (ml + __log2f(sum)) * kLn2 : -INFINITY;
+          if (l.lse && grp == 0) l.lse[row] = sum > 0.f ? (m + __log2f(sum)) * kLn2 : -INFINITY;
         }
       } else {
         const int f = starts ? 1 : 0;   // [1] is the wave's last: its stage is free
 #pragma unroll
         for (int x = 0; x < NX; ++x)
           s_frag[wv][f][64 * x + lane] = make_float4(o[x][0], o[x][1], o[x][2], o[x][3]);
-        if (grp == 0) s_ml[wv][f][col] = make_float2(ml, sum);
+        if (grp == 0) s_ml[wv][f][col] = make_float2(m, sum);
         if (lane == 0) {
           s_meta[wv][f] = make_int4(cur.row, cur.heads, (starts ? 1 : 0) | (ends ? 2 : 0) | 4, 0);
           s_row[wv][f][0] = cur.item_start + (long long)cur.sub * cur.n;
