@@ -513,6 +513,7 @@ ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_to
  *    a problem with the same B and group_size).  group_size must divide
  *    Hq / Hkv; 0 stands for Hq / Hkv.
  *        out = softmax(sm_scale * q.k) . v     (bf16 MFMA, fp32 softmax)
+ *    The softmax weights meet v with 16 bits (two bf16), whatever the heads.
  *    A request that sees no key (kv_len 0, an empty table row) gets out = 0,
  *    lse = -inf; a score of NaN or +inf gives out = NaN, lse = -inf, as in
  *    section 3.  A value that is not finite makes the elements of out that it

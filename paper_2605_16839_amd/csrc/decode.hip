@@ -20,10 +20,11 @@
 //     the KV head being the 16 columns (more than 16 heads: tiles of 16 that read the
 //     pages each).  key_of gives a lane 8 consecutive keys of each 32-key step,
 //     as the P^T fragment wants them; token-major V is read from LDS transposed;
-//   * up to 8 heads leave half of the columns free: they hold the same heads
-//     again, and carry the part of the weights that bf16 loses (p - bf16(p)),
-//     so the weights count with 16 bits at no cost.  With 9 to 16 heads the weights
-//     are rounded to bf16, as the chunk attention's are;
+//   * weights count with 16 bits: bf16(p), and the part of p that it loses as a second
+//     bf16 (p - bf16(p)).  Up to 8 heads leave half of the columns free: they hold
+//     the same heads again, and carry the second part at no cost.  With 9 to 16 heads it takes
+//     a second MFMA on the same V fragment, into sums of its own (454 MB for 16 heads, D =
+//     128: 88.7 us, 85.1 without; transposed V 85.2 and 84.8);
 //   * a row that lies inside one wave's share is written at once; pieces of
 //     a workgroup's waves are joined in its LDS, and rows that several workgroups
 //     share by the last of them (join_row), or by a second launch where few rows may
@@ -324,7 +325,8 @@ struct Part {
   long long item_start;  // the item's first page
 };
 
-// VT: transposed V pages.  DUP: at most 8 heads per tile, see above.
+// VT: transposed V pages.  DUP: at most 8 heads per tile, whose weights' second parts
+// are in the upper columns.
 template <int D, bool VT, bool DUP>
 __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a) {
   constexpr int NX = D / 16, NK = D / 32;      // d tiles, k-steps of a score
@@ -507,7 +509,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
       }
       __builtin_amdgcn_wave_barrier();
     };
-    f32x4 o[NX];
+    constexpr int NR = DUP ? 0 : NX;   // d tiles of the weights' second parts
+    f32x4 o[NX], rest[NR > 0 ? NR : 1];
     // m is carried scaled and rounded, as the weights take it off: while the maximum
     // stays, its factor is 1 exactly.  Scaled anew for every page it would be fused into the
     // difference and leave the product's rounding there, on all earlier pages, every time
@@ -516,6 +519,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
     auto clear = [&] {
 #pragma unroll
       for (int x = 0; x < NX; ++x) o[x] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < NR; ++x) rest[x] = {0.f, 0.f, 0.f, 0.f};
       m = -INFINITY, sum = 0.f;
     };
     clear();
@@ -579,19 +584,22 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
           part += s[t][e];
         }
       sum = __builtin_fmaf(sum, alpha, part);
-      bf16x8 pt[2];
+      bf16x8 pt[2], pr[2];
       const float keep = DUP && col >= 8 ? 1.f : 0.f;
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float x = s[2 * c + (e >> 2)][e & 3];
-          // weights to bf16: to 8 bits, or with the upper columns to 16
+          // weights to 16 bits, in two parts
           const __bf16 hi = (__bf16)x;
           pt[c][e] = DUP ? (__bf16)__builtin_fmaf(-keep, (float)hi, x) : hi;
+          if constexpr (!DUP) pr[c][e] = (__bf16)(x - (float)hi);
         }
 #pragma unroll
       for (int x = 0; x < NX; ++x) o[x] *= alpha;
+#pragma unroll
+      for (int x = 0; x < NR; ++x) rest[x] *= alpha;
       if (id < 0) {
         const int keys = id == -1 ? 0 : cur.last_keys;
         // weights of 0 do not undo a NaN in V
@@ -620,6 +628,12 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
           __builtin_amdgcn_s_barrier();
           ++step;
         }
+        // d tile t of the result, 32-key step c
+        auto add_v = [&](const u32x4& f, int t, int c) {
+          o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pt[c], o[t], 0, 0, 0);
+          if constexpr (!DUP)
+            rest[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pr[c], rest[t], 0, 0, 0);
+        };
         if constexpr (VT) {
 #pragma unroll
           for (int c = 0; c < 2; ++c)
@@ -627,8 +641,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
             for (int y = 0; y < NX / 2; ++y) {
               const u32x4 f = *reinterpret_cast<const u32x4*>(
                   stage + (16 * y + col) * kPage * 2 + 16 * swizzle<D, kHalfVT>(col, 4 * c + grp));
-              f32x4& to = o[h * (NX / 2) + y];
-              to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pt[c], to, 0, 0, 0);
+              add_v(f, h * (NX / 2) + y, c);
             }
         } else {
           const int r0 = 8 * grp + (col >> 2);
@@ -640,7 +653,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
             const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 4 * D * 2));
             const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
             const u32x4 f = {l2[0], l2[1], h2[0], h2[1]};
-            o[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), pt[h], o[y], 0, 0, 0);
+            add_v(f, y, h);
           }
         }
         __builtin_amdgcn_wave_barrier();
@@ -651,11 +664,10 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
 
       // ---- the row's end, or the share's
       sum = groups_sum(sum);
-      if constexpr (DUP)
 #pragma unroll
-        for (int x = 0; x < NX; ++x)
+      for (int x = 0; x < NX; ++x)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[x][e] += other_half(o[x][e]);
+        for (int e = 0; e < 4; ++e) o[x][e] += DUP ? other_half(o[x][e]) : rest[NR > 0 ? x : 0][e];
       const bool starts = cur.p == 0, ends = cur.p + cur.cnt == cur.n;
       if (starts && ends) {
         if (col < cur.heads) {
