@@ -667,7 +667,11 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
 #pragma unroll
       for (int x = 0; x < NX; ++x)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[x][e] += DUP ? other_half(o[x][e]) : rest[NR > 0 ? x : 0][e];
+        for (int e = 0; e < 4; ++e) {
+          // an infinity of v reaches the second parts with any sign, or none (inf * 0)
+          const float second = DUP ? other_half(o[x][e]) : rest[NR > 0 ? x : 0][e];
+          o[x][e] += __builtin_isfinite(o[x][e]) ? second : 0.f;
+        }
       const bool starts = cur.p == 0, ends = cur.p + cur.cnt == cur.n;
       if (starts && ends) {
         if (col < cur.heads) {

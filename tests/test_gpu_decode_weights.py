@@ -70,3 +70,37 @@ def test_weights_keep_16_bits(Hq, Hkv, D, gs, layout):
     tol = BF16_HALF * np.abs(ref) + (2.0 ** -16 + 2 * delta[..., None] + 2.0 ** -20) * mass
     assert (err <= tol).all(), (float((err - tol).max()), np.argwhere(err > tol)[:4].tolist())
     assert (np.abs(lse - ref_lse) <= delta + 2.0 ** -20 * np.maximum(1, np.abs(ref_lse))).all()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 64), (8, 1, 128), (6, 2, 128), (9, 1, 128), (16, 1, 64), (20, 1, 64)])
+def test_infinite_values(Hq, Hkv, D, layout):
+    """out has the infinity of the values that it sums, NaN for both signs or a NaN, in rows of a
+    page, of a wave's pages and of several workgroups' pieces."""
+    rng = np.random.default_rng(Hq)
+    lens = [1, 60, 300, 9000, 64 * 200]
+    kp, vp, table, pages = _cache(rng, lens, Hkv, D)
+    q = _bf16(rng, (len(lens), Hq, D), 0.5)      # every weight is far from 0
+    inf, minus, nan = 0x7f80, 0xff80, 0x7fc0
+    for b, n in enumerate(lens):
+        for h in range(Hkv):
+            def put(pos, d, bits):
+                vp[table[b, h, pos // 64], pos % 64, d] = bits
+            put(0, 1, inf), put(n - 1, 2, minus), put(n // 2, 3, nan)
+            put(0, 5, inf), put(n - 1, 5, inf)
+            put(n // 3, D - 1, minus)
+            if n > 1:
+                put(0, 7, inf), put(n - 1, 7, minus)
+    scale = D ** -0.5
+    got, lse = _decode(q, kp, vp, table, lens, pages, scale, layout)
+    clean = np.where((vp & 0x7f80) == 0x7f80, np.uint16(0), vp)
+    ref, ref_lse, mass, size = serving.decode_attention(q, kp, clean, table, lens, scale)
+    with np.errstate(invalid="ignore"):
+        raw = serving.decode_attention(q, kp, vp, table, lens, scale)[0]
+    at = ~np.isfinite(raw)
+    assert at[..., [1, 2, 3, 5, D - 1]].all() and np.isnan(raw[1:, :, 7]).all()
+    assert np.array_equal(got[at], raw[at], equal_nan=True)
+    delta = D * 2.0 ** -23 * size
+    tol = BF16_HALF * np.abs(ref) + (2.0 ** -16 + 2 * delta[..., None] + 2.0 ** -20) * mass
+    assert (np.abs(got - ref) <= tol)[~at].all()
+    assert (np.abs(lse - ref_lse) <= delta + 2.0 ** -20 * np.maximum(1, np.abs(ref_lse))).all()
