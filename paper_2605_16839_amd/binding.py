@@ -2,7 +2,8 @@
 
 Argument marshalling only: every step of the path runs in the HIP kernels of
 the shared library.  torch is used for device memory and streams; tensors are
-passed by ``data_ptr()`` and every call is enqueued on torch's current stream.
+passed by ``data_ptr()`` and every call is enqueued on torch's current stream, or
+on ``stream=``.
 If the library has not been built, loading fails loudly -- there is no CPU
 fallback.
 """
@@ -186,6 +187,15 @@ def _stream(stream=None):
     return ctypes.c_void_p((stream or torch.cuda.current_stream()).cuda_stream)
 
 
+def _on(stream, fn, arguments: dict):
+    """The call fn(**arguments) with ``stream`` as the current one, so that what the call makes,
+    workspaces and outputs, comes from that stream's memory and is filled there.  From the
+    caller's stream it could be memory that work there still uses, and a workspace let go at
+    the end would be given out again while the kernels run."""
+    with torch.cuda.stream(stream):
+        return fn(**{**arguments, "stream": None})
+
+
 class Problem:
     """Sizes of one chunk step plus the per-sequence cached lengths.
 
@@ -250,6 +260,8 @@ def _dev(p: Problem):
 
 
 def pool_q_blocks(p: Problem, q: torch.Tensor, q_mean: Optional[torch.Tensor] = None, stream=None):
+    if stream is not None:
+        return _on(stream, pool_q_blocks, locals())
     if q_mean is None:
         q_mean = torch.empty((p.batch, p.num_q_heads, p.n_qblocks, p.head_dim),
                              dtype=torch.float32, device=q.device)
@@ -259,6 +271,8 @@ def pool_q_blocks(p: Problem, q: torch.Tensor, q_mean: Optional[torch.Tensor] = 
 
 def pool_k_blocks(p: Problem, k_pool: torch.Tensor, page_table: torch.Tensor,
                   k_mean: Optional[torch.Tensor] = None, first_block: int = 0, stream=None):
+    if stream is not None:
+        return _on(stream, pool_k_blocks, locals())
     if k_mean is None:
         k_mean = torch.zeros((p.batch, p.num_kv_heads, p.max_kv_blocks, p.head_dim),
                              dtype=torch.float32, device=k_pool.device)
@@ -269,6 +283,8 @@ def pool_k_blocks(p: Problem, k_pool: torch.Tensor, page_table: torch.Tensor,
 
 def block_scores(p: Problem, q_mean: torch.Tensor, k_mean: torch.Tensor,
                  scores: Optional[torch.Tensor] = None, stream=None):
+    if stream is not None:
+        return _on(stream, block_scores, locals())
     if scores is None:
         scores = torch.full((p.batch, p.num_q_heads, p.n_qblocks, p.max_kv_blocks), float("nan"),
                             dtype=torch.float32, device=q_mean.device)
@@ -279,6 +295,8 @@ def block_scores(p: Problem, q_mean: torch.Tensor, k_mean: torch.Tensor,
 
 def select_blocks(p: Problem, scores: torch.Tensor, top_frac: float, sink_blocks: int = 1,
                   local_blocks: int = 4, masks: Optional[torch.Tensor] = None, stream=None):
+    if stream is not None:
+        return _on(stream, select_blocks, locals())
     if masks is None:
         masks = torch.empty((p.batch, p.num_q_heads, p.n_qblocks, p.words), dtype=torch.int64,
                             device=scores.device)
@@ -292,6 +310,8 @@ def estimate_masks(p: Problem, q: torch.Tensor, k_pool: torch.Tensor, page_table
                    k_mean: Optional[torch.Tensor] = None, k_mean_first_block: int = 0,
                    bufs: Optional[dict] = None, stream=None):
     """Returns (masks int64-bits [B,Hq,nQB,W], dict of q_mean, k_mean, scores)."""
+    if stream is not None:
+        return _on(stream, estimate_masks, locals())
     dev = q.device
     b = bufs if bufs is not None else {}
     if "q_mean" not in b:
@@ -321,6 +341,8 @@ def estimate_masks_threshold(p: Problem, q: torch.Tensor, k_pool: torch.Tensor,
                              k_mean: Optional[torch.Tensor] = None, k_mean_first_block: int = 0,
                              bufs: Optional[dict] = None, stream=None):
     """Alpha-threshold selector: (masks, buffers) like estimate_masks."""
+    if stream is not None:
+        return _on(stream, estimate_masks_threshold, locals())
     dev = q.device
     b = bufs if bufs is not None else {}
     if "q_mean" not in b:
@@ -349,6 +371,8 @@ def estimate_masks_threshold(p: Problem, q: torch.Tensor, k_pool: torch.Tensor,
 def select_blocks_threshold(p: Problem, scores: torch.Tensor, alpha: float, temperature: float,
                             sm_scale: float, sink_blocks: int = 1, local_blocks: int = 4,
                             masks: Optional[torch.Tensor] = None, stream=None):
+    if stream is not None:
+        return _on(stream, select_blocks_threshold, locals())
     if masks is None:
         masks = torch.empty((p.batch, p.num_q_heads, p.n_qblocks, p.words), dtype=torch.int64,
                             device=scores.device)
@@ -366,6 +390,8 @@ def build_block_tables(p: Problem, masks: torch.Tensor, group_size: int,
                        out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
                        ws: Optional[torch.Tensor] = None, stream=None):
     """masks -> tables = (kv_indptr [B*G+1], kv_indices [B*G*max_kv_blocks]) int32."""
+    if stream is not None:
+        return _on(stream, build_block_tables, locals())
     dev = masks.device
     R = p.batch * p.n_groups(group_size)
     if out is None:
@@ -385,6 +411,8 @@ def build_block_tables_noalloc(p: Problem, masks: torch.Tensor, group_size: int,
                                stream=None):
     """build_block_tables without a workspace (the library's fixed scratch); the
     caller still owns the output tables (allocated here when ``out`` is None)."""
+    if stream is not None:
+        return _on(stream, build_block_tables_noalloc, locals())
     R = p.batch * p.n_groups(group_size)
     if out is None:
         out = (torch.empty(R + 1, dtype=torch.int32, device=masks.device),
@@ -401,6 +429,8 @@ def estimate_tables(p: Problem, q: torch.Tensor, k_pool: torch.Tensor, page_tabl
                     out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
                     ws: Optional[torch.Tensor] = None, stream=None):
     """Fused estimator -> union -> CSR: returns (tables, buffers); no masks."""
+    if stream is not None:
+        return _on(stream, estimate_tables, locals())
     dev = q.device
     b = bufs if bufs is not None else {}
     if "q_mean" not in b:
@@ -453,6 +483,8 @@ def chunk_attention(p: Problem, q_chunk: torch.Tensor, kv_pool: Tuple[torch.Tens
 
     ``kv_pool`` = (k_pool ``[P, page, D]``, v_pool ``[P, page, D]``, or
     ``[P, D, page]`` when ``p.v_layout == V_TRANSPOSED``)."""
+    if stream is not None:
+        return _on(stream, chunk_attention, locals())
     k_pool, v_pool = kv_pool
     if out is None:
         out = torch.empty_like(q_chunk)
@@ -470,6 +502,8 @@ def dense_paged_chunk_attention(p: Problem, q_chunk: torch.Tensor,
                                 out: Optional[torch.Tensor] = None,
                                 lse: Optional[torch.Tensor] = None,
                                 ws: Optional[torch.Tensor] = None, stream=None):
+    if stream is not None:
+        return _on(stream, dense_paged_chunk_attention, locals())
     k_pool, v_pool = kv_pool
     if out is None:
         out = torch.empty_like(q_chunk)
@@ -491,6 +525,8 @@ def build_block_sparse_tables(p: Problem, masks: torch.Tensor, group_size: int =
                               ws: Optional[torch.Tensor] = None, stream=None):
     """One table per (b, h, Q-block) row: its own mask row (group_size = 0) or the
     causally limited union of its execution group (group_size > 0)."""
+    if stream is not None:
+        return _on(stream, build_block_sparse_tables, locals())
     dev = masks.device
     R = p.batch * p.num_q_heads * p.n_qblocks
     if out is None:
@@ -513,6 +549,8 @@ def block_sparse_chunk_attention(p: Problem, q_chunk: torch.Tensor,
                                  lse: Optional[torch.Tensor] = None,
                                  ws: Optional[torch.Tensor] = None, stream=None):
     """Attention of every (head, Q-block) over its own mask row's blocks."""
+    if stream is not None:
+        return _on(stream, block_sparse_chunk_attention, locals())
     k_pool, v_pool = kv_pool
     if out is None:
         out = torch.empty_like(q_chunk)
@@ -530,6 +568,8 @@ def gather_selected_pages(p: Problem, kv_pool: Tuple[torch.Tensor, torch.Tensor]
                           group_size: int, capacity_pages: Optional[int] = None,
                           out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None):
     """Copy arm: pack every group's selected K/V pages contiguously in table order."""
+    if stream is not None:
+        return _on(stream, gather_selected_pages, locals())
     k_pool, v_pool = kv_pool
     if capacity_pages is None:
         capacity_pages = p.batch * p.n_groups(group_size) * p.max_kv_blocks
@@ -552,6 +592,8 @@ def packed_chunk_attention(p: Problem, q_chunk: torch.Tensor,
                            out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                            ws: Optional[torch.Tensor] = None, stream=None):
     """Copy arm: attention over the packed pools (table entry p = packed page p)."""
+    if stream is not None:
+        return _on(stream, packed_chunk_attention, locals())
     k_packed, v_packed = packed
     if out is None:
         out = torch.empty_like(q_chunk)
@@ -579,6 +621,8 @@ def check_tables_host(p: Problem, group_size: int, kv_indptr, kv_indices, page_t
 
 def validate_tables(p: Problem, group_size: int, tables, require_chunk_open: bool = True,
                     stream=None) -> None:
+    if stream is not None:
+        return _on(stream, validate_tables, locals())
     _check(load().ca_validate_tables(p.ref, group_size, _ptr(tables[0]), _ptr(tables[1]),
                                      int(require_chunk_open), _stream(stream)))
 
@@ -635,16 +679,16 @@ def _need(name: str, t: torch.Tensor, dtype: torch.dtype, shape: tuple, index: i
     return t.data_ptr()
 
 
-def _here(t: torch.Tensor, stream):
+def _here(t: torch.Tensor):
     """A call's device index and stream: tensors have to be on the current device, whose
     stream the call is enqueued on."""
     index = t.get_device()
     if index < 0 or index != torch.cuda.current_device():
         raise ValueError(f"tensors on {t.device}: they must be on the current device"
                          + (f", cuda:{torch.cuda.current_device()}" if index >= 0 else ""))
-    if stream is None and _raw_stream is not None:
+    if _raw_stream is not None:
         return index, _raw_stream(index)
-    return index, (stream or torch.cuda.current_stream()).cuda_stream
+    return index, torch.cuda.current_stream().cuda_stream
 
 
 def check_cache(c: Cache, group_size: int = 0) -> None:
@@ -659,7 +703,9 @@ def assign_slots(c: Cache, new_len: torch.Tensor, num_tokens: int, seq_len: torc
     Returns ``bufs`` (made where missing): slot_map int64 [num_tokens, Hkv], and int32
     positions [num_tokens], token_indptr [B + 1], granted [B], seq_len [B] and
     free_count [1] after the step; the last two may be the inputs themselves."""
-    index, st = _here(new_len, stream)
+    if stream is not None:
+        return _on(stream, assign_slots, locals())
+    index, st = _here(new_len)
     i32, B, T = torch.int32, c.batch, num_tokens
     new = _need("new_len", new_len, i32, (B,), index)
     b = bufs if bufs is not None else {}
@@ -696,7 +742,9 @@ def release_pages(c: Cache, release: torch.Tensor, seq_len: torch.Tensor,
                   out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None):
     """Ends the requests with release != 0: their pages go behind the free ones in free_pages.
     Returns (seq_len, free_count) after it, which may be the inputs themselves (``out``)."""
-    index, st = _here(release, stream)
+    if stream is not None:
+        return _on(stream, release_pages, locals())
+    index, st = _here(release)
     i32, B = torch.int32, c.batch
     lens, count = _need("seq_len", seq_len, i32, (B,), index), _need("free_count", free_count, i32, (1,), index)
     if out is None:
@@ -729,7 +777,9 @@ def rotary_append(c: Cache, r: Rotary, q: torch.Tensor, k: torch.Tensor, v: torc
     """Rotates q [T, Hq, D] and k [T, Hkv, D] by their positions ([T], or [axes, T]) and writes
     keys and values to slot_map's places in the pools; returns the rotated queries.  q, k and v
     may be parts of one tensor (a token's heads together, tokens apart)."""
-    index, st = _here(q, stream)
+    if stream is not None:
+        return _on(stream, rotary_append, locals())
+    index, st = _here(q)
     bf = torch.bfloat16
     T, Hq, Hkv, D = q.shape[0], c.num_q_heads, c.num_kv_heads, c.head_dim
     qp, qs = _rows("q", q, (T, Hq, D), index)
@@ -763,7 +813,9 @@ def decode_attention(c: Cache, q: torch.Tensor, kv_pool: Tuple[torch.Tensor, tor
     """Attention of one new token per request, q [B, Hq, D], over its kv_len[b] cached tokens, or
     over the blocks that ``tables`` (kv_indptr, kv_indices; one row per group of group_size heads,
     0: all heads of a KV head) list; returns (out bf16, lse fp32 or None)."""
-    index, st = _here(q, stream)
+    if stream is not None:
+        return _on(stream, decode_attention, locals())
+    index, st = _here(q)
     bf, i32 = torch.bfloat16, torch.int32
     shape = (c.batch, c.num_q_heads, c.head_dim)
     qp = _need("q", q, bf, shape, index)
