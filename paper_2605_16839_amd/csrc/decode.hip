@@ -664,14 +664,27 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
 
       // ---- the row's end, or the share's
       sum = groups_sum(sum);
+      // an infinity of v reaches the second parts with any sign, or none (inf * 0)
+      float far = 0.f;
 #pragma unroll
       for (int x = 0; x < NX; ++x)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          // an infinity of v reaches the second parts with any sign, or none (inf * 0)
-          const float second = DUP ? other_half(o[x][e]) : rest[NR > 0 ? x : 0][e];
-          o[x][e] += __builtin_isfinite(o[x][e]) ? second : 0.f;
-        }
+        for (int e = 0; e < 4; ++e) far = max2(far, __builtin_fabsf(o[x][e]));
+      const bool finite = __ballot(!(far < INFINITY)) == 0;
+      if (__builtin_expect(!finite, 0)) {   // out of the way: code is cold at a row's end
+#pragma unroll
+        for (int x = 0; x < NX; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float second = DUP ? other_half(o[x][e]) : rest[NR > 0 ? x : 0][e];
+            o[x][e] += __builtin_isfinite(o[x][e]) ? second : 0.f;
+          }
+      } else {
+#pragma unroll
+        for (int x = 0; x < NX; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[x][e] += DUP ? other_half(o[x][e]) : rest[NR > 0 ? x : 0][e];
+      }
       const bool starts = cur.p == 0, ends = cur.p + cur.cnt == cur.n;
       if (starts && ends) {
         if (col < cur.heads) {
