@@ -522,7 +522,10 @@ ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_to
  *    kv_len is taken as 0 below 0 and as 64 * max_kv_blocks above it; blocks
  *    whose table entry or page id is out of range add no keys.
  *    Workspace: ca_decode_workspace_bytes(c, group_size) bytes, 16-byte aligned,
- *    whatever it holds; calls that may overlap must not share one.
+ *    whatever it holds; calls that may overlap must not share one.  (Had a captured
+ *    call run at once with another on its workspace, or while kv_len was written, fill
+ *    the workspace with zeros before its next replay: a replay cannot tell its
+ *    own earlier counts of pieces from the present ones.)
  * ---------------------------------------------------------------------- */
 size_t ca_decode_workspace_bytes(const ca_cache* c, int32_t group_size);
 

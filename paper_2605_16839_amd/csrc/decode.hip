@@ -30,6 +30,7 @@
 //     share by the last of them (join_row), or by a second launch where few rows may
 //     be in many pieces (decode_join_kernel).  Pieces are taken in page order, so
 //     the result does not depend on who is last.
+#include <atomic>
 #include <cstdint>
 #include <type_traits>
 
@@ -58,6 +59,7 @@ struct DecodeArgs {
   float* part_o;                    // [kGroups][2][16][D]
   float* part_ml;                   // [kGroups][2][16][2]: maximum (log2 units) and sum
   unsigned long long* arrived;      // [kGroups]: pieces there are of the row that starts in a share
+  unsigned long long piece;         // what a piece counts, see last_of
   bool join_later;                  // decode_join_kernel joins the rows
 };
 
@@ -202,26 +204,30 @@ __device__ __forceinline__ float2 get2(const float* p) {
   return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
 
-// Counts a piece of a row in; true for the last of n.  A counter is kCounter plus
-// the pieces so far, and plain kCounter between launches.  A workspace may hold
-// anything at first: who finds a value that is no counter makes it one, with a swap
-// that only one of those who find it can win, and counts in if it is another.
-constexpr unsigned long long kCounter = 0x5ca1ab1e'0dd5'0000ull;
-__device__ __forceinline__ bool last_of(unsigned long long* counter, int n) {
+// Counts a piece of a row in; true for the last of n.  A counter is 0 between launches,
+// and each piece adds `piece`, a number of this launch with 1 in the low 16 bits: k pieces
+// are k * piece, which no other number of pieces of no other launch is.  A workspace may hold
+// anything at first, the counts of an earlier launch too whose pieces never came together:
+// who finds a value that is no count of this launch makes it one, with a swap that only
+// one of those who find it can win, and counts in if it is another.
+constexpr unsigned long long kLaunchTop = 0xa7ull << 40;   // above the 40 bits of a launch's number
+__device__ __forceinline__ bool last_of(unsigned long long* counter, unsigned long long piece, int n) {
+  const unsigned long long others = (unsigned long long)(n - 1) * piece;   // while the add is on its way
+  auto counts = [&](unsigned long long v) { return (int)(v & 0xffff) < n && v == (v & 0xffff) * piece; };
   unsigned long long was =
-      __hip_atomic_fetch_add(counter, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  while ((was ^ kCounter) >> 16) {
+      __hip_atomic_fetch_add(counter, piece, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  while (__builtin_expect(was != others && !counts(was), 0)) {
     unsigned long long now = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if ((now ^ kCounter) >> 16) {
-      if (__hip_atomic_compare_exchange_strong(counter, &now, kCounter + 1, __ATOMIC_RELAXED,
+    if (!counts(now)) {
+      if (__hip_atomic_compare_exchange_strong(counter, &now, piece, __ATOMIC_RELAXED,
                                                __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
-        was = kCounter;
+        was = 0;
     } else {
-      was = __hip_atomic_fetch_add(counter, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      was = __hip_atomic_fetch_add(counter, piece, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   }
-  if ((int)(was & 0xffff) != n - 1) return false;
-  __hip_atomic_store(counter, kCounter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (was != others) return false;
+  __hip_atomic_store(counter, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return true;
 }
 
@@ -805,7 +811,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
     __syncthreads();
     if (tid < 2) {
       const int w0 = tid ? left_w0[1] : left_w0[0], w1 = tid ? left_w1[1] : left_w1[0];
-      s_last[tid] = w0 >= 0 && last_of(a.arrived + w0, w1 - w0 + 1);
+      s_last[tid] = w0 >= 0 && last_of(a.arrived + w0, a.piece, w1 - w0 + 1);
     }
     JoinSpace& space = *reinterpret_cast<JoinSpace*>(&s_frag[0][0][0]);
     __syncthreads();
@@ -929,6 +935,8 @@ hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& l, hipStream_t 
   a.part_o = static_cast<float*>(l.ws);
   a.part_ml = a.part_o + (size_t)kGroups * 2 * kTileHeads * d.D;
   a.arrived = reinterpret_cast<unsigned long long*>(a.part_ml + (size_t)kGroups * 2 * kTileHeads * 2);
+  static std::atomic<unsigned long long> launches{0};
+  a.piece = (kLaunchTop | (launches.fetch_add(1, std::memory_order_relaxed) & 0xff'ffff'ffffull)) << 16 | 1;
   // a row of at most 64 pieces (32 and fewer as a rule) is joined in the launch, whatever the rows
   a.join_later = (long long)a.items * a.per_item <= kFewRows && a.max_kv_blocks > kManyPieces;
   const bool vt = d.v_layout != 0;
