@@ -61,3 +61,74 @@ def test_a_maximum_that_stays(top, layout):
     # values: two sums with as many roundings, weights of 16 bits
     tol = BF16_HALF * np.abs(ref) + (2.0 ** -16 + 4 * (pages + 28) * 2.0 ** -24) * mass
     assert (np.abs(bf16_host_f64(out) - ref) <= tol).all()
+
+
+def _check(rng, lens, Hq, Hkv, D, layout, most, pool, sample, tables=None, gs=0):
+    """Every request's pages are drawn from a small pool; a sample of requests against the oracle,
+    all rows against a second call."""
+    B = len(lens)
+    kp, vp = (synth.bf16_round(rng.standard_normal((pool, 64, D)).astype(np.float32)) for _ in "kv")
+    q = synth.bf16_round(rng.standard_normal((B, Hq, D)).astype(np.float32))
+    table = rng.integers(0, pool, (B, Hkv, most))
+    c = ca.Cache(B, Hq, Hkv, D, most, pool, v_layout=layout)
+    lse = torch.empty(B, Hq, device=DEV)
+    csr = None
+    if tables:
+        rows = [r for t in tables for r in t]
+        ip = np.concatenate([[0], np.cumsum([len(r) for r in rows])])
+        ix = np.zeros(len(rows) * most)
+        ix[:ip[-1]] = [j for r in rows for j in r]
+        csr = (i32_dev(ip), i32_dev(ix))
+    args = (c, bf16_dev(q), (bf16_dev(kp), bf16_dev(vp if layout == 0 else synth.v_pages_transposed(vp))),
+            i32_dev(table), i32_dev(lens), D ** -0.5)
+    out, _ = ca.decode_attention(*args, lse=lse, tables=csr, group_size=gs)
+    again, _ = ca.decode_attention(*args, tables=csr, group_size=gs)
+    assert torch.equal(out, again)
+    sample = list(sample)
+    ref, ref_lse, mass, size = serving.decode_attention(q[sample], kp, vp, table[sample], [lens[b] for b in sample],
+                                                        D ** -0.5, [tables[b] for b in sample] if tables else None, gs)
+    got, gl = bf16_host_f64(out)[sample], lse.cpu().numpy().astype(np.float64)[sample]
+    pages = sum(-(-n // 64) for n in lens) * Hkv / WAVES + 1
+    delta = D * 2.0 ** -23 * size
+    steps = (pages + 28) * 2.0 ** -24
+    tol = BF16_HALF * np.abs(ref) + (2.0 ** -16 + 2 * delta[..., None] + 4 * steps) * mass
+    assert (np.abs(got - ref) <= tol).all(), np.argwhere(np.abs(got - ref) > tol)[:5].tolist()
+    fin = np.isfinite(ref_lse)
+    assert np.array_equal(gl[~fin], ref_lse[~fin])
+    assert (np.abs(gl - ref_lse) <= delta + 4 * 2.0 ** -24 * np.abs(ref_lse) + steps)[fin].all()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 8, 64), (16, 4, 128), (12, 1, 64), (18, 2, 128)])
+def test_more_than_64_pages_to_a_wave(Hq, Hkv, D, layout):
+    """Page ids are fetched 64 at a time: rows of about as many, and of many more, in shares of
+    more than 128 pages that they begin, end and cross."""
+    rng = np.random.default_rng(Hq)
+    blocks = [63, 64, 65, 1, 127, 128, 129, 2, 191, 192, 193, 700, 62, 66, 1023]
+    B = 2600 // Hkv
+    take = rng.integers(0, len(blocks), B)
+    lens = [64 * blocks[i] - int(rng.integers(0, 64)) for i in take]
+    lens[0], lens[B - 1], lens[7] = 64 * 1024, 64 * 65, 0
+    assert sum(-(-n // 64) for n in lens) * Hkv > 128 * WAVES
+    sample = sorted({0, 7, B - 1, *rng.choice(B, 8, replace=False).tolist()})
+    _check(rng, lens, Hq, Hkv, D, layout, 1024, 300, sample)
+
+
+def test_more_than_64_pages_to_a_wave_of_few_requests():
+    """One lane to a request."""
+    rng = np.random.default_rng(3)
+    lens = [64 * int(n) - 5 for n in rng.integers(500, 4000, 40)]
+    for layout in (0, 1):
+        _check(rng, lens, 8, 4, 64, layout, 4096, 200, [0, 11, 39])
+
+
+def test_more_than_64_listed_pages_to_a_wave():
+    rng = np.random.default_rng(4)
+    B, Hq, Hkv, gs, most = 128, 16, 8, 1, 512
+    lens = [64 * most - 7] * B
+    some = [sorted(rng.choice(most, int(n), replace=False).tolist()) for n in (63, 64, 65, 129, 200, 511, 512, 0)]
+    tables = [[some[int(i)] for i in rng.integers(0, len(some), Hq // gs)] for _ in range(B)]
+    tables[5][3] = some[6]
+    assert sum(len(r) for t in tables for r in t) > 96 * WAVES
+    for layout in (0, 1):
+        _check(rng, lens, Hq, Hkv, 64, layout, most, 200, [0, 5, 77, 127], tables, gs)
