@@ -442,7 +442,19 @@ __global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a)
     if (sub == a.per_item) {
       sub = 0;
       item_start += (long long)n * a.per_item;
-      do n = ++item < a.items ? pages_of(item) : -1; while (n == 0);
+      if (per == 1) {
+        do n = ++item < a.items ? pages_of(item) : -1; while (n == 0);
+      } else {   // 64 at a time: 1000 idle requests would be as many loads one after the other
+        n = -1;
+        for (int i = item + 1; n < 0 && i < a.items; i += kWave) {
+          const int here = i + lane < a.items ? item_pages(a, i + lane) : 0;
+          const unsigned long long hit = __ballot(here > 0);
+          if (!hit) continue;
+          const int k = __builtin_ctzll(hit);
+          item = i + k;
+          n = __builtin_amdgcn_readlane(here, k);
+        }
+      }
       if (n < 0) item = t.item, n = 1;   // only if the lengths changed under the kernel
     }
     return part_of(item, sub, n, 0, left, item_start);

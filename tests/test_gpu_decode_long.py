@@ -132,3 +132,17 @@ def test_more_than_64_listed_pages_to_a_wave():
     assert sum(len(r) for t in tables for r in t) > 96 * WAVES
     for layout in (0, 1):
         _check(rng, lens, Hq, Hkv, 64, layout, most, 200, [0, 5, 77, 127], tables, gs)
+
+
+@pytest.mark.parametrize("gap", [1, 62, 63, 64, 65, 127, 128, 1000])
+def test_idle_requests_inside_a_share(gap):
+    """A wave goes from one request to the next over those that have nothing."""
+    rng = np.random.default_rng(gap)
+    lens = [64 * 401 + 5] + [0] * gap + [64 * 200] + [0] * gap + [64 * 399 - 1, 3] + [0] * gap
+    live = [0, gap + 1, 2 * gap + 2, 2 * gap + 3]
+    sample = [0, 1, gap, gap + 1, gap + 2, *live[2:], len(lens) - 1]
+    _check(rng, lens, 16, 8, 64, gap % 2, 402, 500, sample)
+    # over tables: rows of no block between rows of some
+    B, Hq, gs = 3, 256, 1
+    rows = [[list(range(90))] + [[]] * (Hq - 2) + [list(range(7, 96))] for _ in range(B)]
+    _check(rng, [64 * 96] * B, Hq, 4, 64, gap % 2, 96, 300, range(B), rows, gs)
