@@ -63,7 +63,8 @@ __device__ __forceinline__ void transposed_tile(const AppendArgs& a, int tile, T
     if (slot < 0 || slot >= a.num_slots) slot = -1;
     s.slot[tid] = slot;
     // follows: the next token has the next slot
-    const unsigned long long follows = __ballot(slot >= 0 && __shfl_down(slot, 1, kWave) == slot + 1);
+    const long long next = __shfl_down(slot, 1, kWave);   // of every lane, so before any condition
+    const unsigned long long follows = __ballot(slot >= 0 && next == slot + 1);
     const bool starts = slot >= 0 && slot % 8 == 0 && tid <= kTileTokens - 8 &&
                         ((follows >> tid) & 0x7f) == 0x7f;
     const unsigned long long runs = __ballot(starts);
