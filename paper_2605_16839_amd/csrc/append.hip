@@ -49,7 +49,9 @@ constexpr int kTileDims = 64;
 struct Tile {
   uint32_t v[kTileTokens][kTileDims / 2 + 1];   // + 1: 8 tokens on is 8 banks on
   long long slot[kTileTokens];
-  unsigned long long runs, alone;   // bit i: a run starts at token i; token i is in none
+  int runs, alone;                  // how many there are, and
+  uint8_t run[kTileTokens / 8];     // the first token of each run,
+  uint8_t lone[kTileTokens];        // the tokens that are in none
 };
 __device__ __forceinline__ void transposed_tile(const AppendArgs& a, int tile, Tile& s) {
   const AppendLaunch& l = a.l;
@@ -71,7 +73,10 @@ __device__ __forceinline__ void transposed_tile(const AppendArgs& a, int tile, T
     unsigned long long in = runs;   // runs do not overlap: they start 8 slots apart
     in |= in << 1, in |= in << 2, in |= in << 4;
     const unsigned long long alone = __ballot(slot >= 0) & ~in;
-    if (tid == 0) s.runs = runs, s.alone = alone;
+    const unsigned long long before = (1ull << tid) - 1;
+    if (starts) s.run[__popcll(runs & before)] = tid;
+    if ((alone >> tid) & 1) s.lone[__popcll(alone & before)] = tid;
+    if (tid == 0) s.runs = __popcll(runs), s.alone = __popcll(alone);
   }
   const uint16_t* const src = l.v + t0 * l.v_stride + (long long)head * a.D + slice * kTileDims;
 #pragma unroll
@@ -88,13 +93,10 @@ __device__ __forceinline__ void transposed_tile(const AppendArgs& a, int tile, T
     return l.v_pool + (slot / kPage) * (kPage * a.D) + (long long)(slice * kTileDims + d) * kPage + slot % kPage;
   };
   // two dimensions of a run: neighbouring threads take neighbouring runs
-  const int runs = __popcll(s.runs);
   for (int w = tid; w < 8 * (kTileDims / 2); w += kAppendThreads) {
     const int r = w % 8, p = w / 8;
-    if (r >= runs) continue;
-    unsigned long long m = s.runs;
-    for (int i = 0; i < r; ++i) m &= m - 1;
-    const int i0 = __builtin_ctzll(m);
+    if (r >= s.runs) continue;
+    const int i0 = s.run[r];
     u32x4 lo, hi;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -105,12 +107,8 @@ __device__ __forceinline__ void transposed_tile(const AppendArgs& a, int tile, T
     *reinterpret_cast<u32x4*>(row(s.slot[i0], 2 * p)) = lo;
     *reinterpret_cast<u32x4*>(row(s.slot[i0], 2 * p + 1)) = hi;
   }
-  const int alone = __popcll(s.alone);
-  for (int w = tid; w < alone * (kTileDims / 2); w += kAppendThreads) {
-    const int k = w / (kTileDims / 2), p = w % (kTileDims / 2);
-    unsigned long long m = s.alone;
-    for (int i = 0; i < k; ++i) m &= m - 1;
-    const int i = __builtin_ctzll(m);
+  for (int w = tid; w < s.alone * (kTileDims / 2); w += kAppendThreads) {
+    const int i = s.lone[w / (kTileDims / 2)], p = w % (kTileDims / 2);
     const uint32_t x = s.v[i][p];
     uint16_t* const to = row(s.slot[i], 2 * p);
     to[0] = (uint16_t)x;
@@ -215,9 +213,12 @@ __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const App
 hipError_t launch_rotary_append(const CacheDims& d, const AppendLaunch& l, hipStream_t st) {
   if (l.num_tokens == 0) return hipSuccess;
   AppendArgs a{l, d.Hq, d.Hkv, d.D, (long long)d.num_pages * kPage, d.v_layout != 0, 0};
-  // tiles where the tokens make enough of them; a decode step's tokens, which lie
-  // in a page each, leave 2 bytes at a time either way (256 of them: 11.0 us without
-  // tiles, 13.7 with; 2048 of a prompt 18.2 and 11.2)
+  // Tiles pay where tokens lie in runs, which the host does not know; by their number a
+  // prompt's chunk and a decode step's tokens, which lie in a page each, are told apart.
+  // 32/8 heads, D = 128, without tiles and with: 512 tokens of a prompt 8.1 and 4.7 us, 2048
+  // 18.7 and 10.7, 512 requests of 4 tokens 33.7 and 16.5; 512 single tokens 10.7 and 11.2, 2048
+  // of them 35.6 and 34.9 (4/1 heads 4.3 and 5.5, 7.5 and 8.3).  Below, 256 of a prompt 5.9
+  // and 4.1, and 64 single tokens, an ordinary step, 4.9 and 5.5.
   const long long tiles = (long long)(l.num_tokens + kTileTokens - 1) / kTileTokens * d.Hkv * (d.D / kTileDims);
   if (a.v_transposed && l.num_tokens >= kMinTileTokens && tiles <= 1 << 22) a.v_tiles = (int)tiles;
   rotary_append_kernel<<<a.v_tiles + l.num_tokens, kAppendThreads, 0, st>>>(a);
