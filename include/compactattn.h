@@ -521,7 +521,8 @@ ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_to
  *    B x max_kv_blocks (with tables: x groups) must be below 2^31.
  *    kv_len is taken as 0 below 0 and as 64 * max_kv_blocks above it; blocks
  *    whose table entry or page id is out of range add no keys.
- *    Workspace: ca_decode_workspace_bytes(c, group_size) bytes, 16-byte aligned,
+ *    Workspace: ca_decode_workspace_bytes(c, group_size) bytes (they go by head_dim
+ *    alone; group_size is checked, 0 bytes if it is refused), 16-byte aligned,
  *    whatever it holds; calls that may overlap must not share one.  (Had a captured
  *    call run at once with another on its workspace, or while kv_len was written, fill
  *    the workspace with zeros before its next replay: a replay cannot tell its

@@ -1053,7 +1053,7 @@ ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_to
 size_t ca_decode_workspace_bytes(const ca_cache* c, int32_t group_size) {
   ca::CacheDims d;
   if (group_size < 0 || check_cache(c, group_size, &d) != CA_OK) return 0;
-  return ca::decode_ws_bytes(d, group_size > 0 ? group_size : d.Hq / d.Hkv);
+  return ca::decode_ws_bytes(d);
 }
 
 ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16_t* k_pool,
@@ -1079,7 +1079,7 @@ ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16
   if ((long long)d.B * (kv_indptr ? d.Hq / gs : 1) * d.max_kv_blocks > INT32_MAX)
     return fail(CA_ERR_SHAPE, "the rows' blocks (batch x max_kv_blocks, with tables x groups) "
                 "must be fewer than 2^31");
-  const size_t need = ca::decode_ws_bytes(d, gs);
+  const size_t need = ca::decode_ws_bytes(d);
   if (need > 0 && (ws == nullptr || ws_bytes < need))
     return fail(CA_ERR_WORKSPACE, "decode attention needs %zu workspace bytes, got %zu", need,
                 ws == nullptr ? (size_t)0 : ws_bytes);

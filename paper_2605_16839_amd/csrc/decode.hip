@@ -926,7 +926,7 @@ hipError_t launch(const DecodeArgs& a, hipStream_t st) {
 
 }  // namespace
 
-size_t decode_ws_bytes(const CacheDims& d, int) {
+size_t decode_ws_bytes(const CacheDims& d) {
   return (size_t)kGroups * (2 * kTileHeads * (d.D * sizeof(float) + sizeof(float2)) +
                            sizeof(unsigned long long));
 }

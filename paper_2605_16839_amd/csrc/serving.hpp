@@ -61,7 +61,7 @@ struct DecodeLaunch {
   int group_size;
   float sm_scale;
 };
-size_t decode_ws_bytes(const CacheDims& d, int group_size);
+size_t decode_ws_bytes(const CacheDims& d);
 hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& a, hipStream_t st);
 
 }  // namespace ca
