@@ -147,3 +147,30 @@ def test_idle_requests_inside_a_share(gap):
     B, Hq, gs = 3, 256, 1
     rows = [[list(range(90))] + [[]] * (Hq - 2) + [list(range(7, 96))] for _ in range(B)]
     _check(rng, [64 * 96] * B, Hq, 4, 64, gap % 2, 96, 300, range(B), rows, gs)
+
+
+def test_idle_requests_inside_a_share_cost_little():
+    """4000 idle requests between two live ones, three times: one load after the other for each of them
+    took 16 times the batch without them; 64 at a time take 3 times."""
+    Hq, Hkv, D, pool = 16, 8, 64, 500
+    live = [64 * 401 + 5, 64 * 200, 64 * 399 - 1, 3]
+    took = []
+    for gap in (70, 4000):     # without a gap there are 70 idle ones behind
+        lens = live + [0] * gap if gap == 70 else [x for n in live[:3] for x in [n] + [0] * gap] + [3]
+        B = len(lens)
+        c = ca.Cache(B, Hq, Hkv, D, 402, pool)
+        pools = tuple(torch.zeros(pool, 64, D, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+        q = torch.zeros(B, Hq, D, dtype=torch.bfloat16, device=DEV)
+        table, kl = torch.zeros(B, Hkv, 402, dtype=torch.int32, device=DEV), i32_dev(lens)
+        out, ws = torch.empty_like(q), torch.zeros(ca.decode_workspace_bytes(c), dtype=torch.uint8, device=DEV)
+        best = float("inf")
+        for _ in range(20):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in "ab")
+            a.record()
+            for _ in range(10):
+                ca.decode_attention(c, q, pools, table, kl, 0.125, out=out, ws=ws)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        took.append(best)
+    assert took[1] < 8 * took[0], took
