@@ -517,7 +517,8 @@ ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_to
  *    A request that sees no key (kv_len 0, an empty table row) gets out = 0,
  *    lse = -inf; a score of NaN or +inf gives out = NaN, lse = -inf, as in
  *    section 3.  A value that is not finite makes the elements of out that it
- *    reaches not finite: infinities of one sign give it, others NaN.  The keys past kv_len may hold anything, NaN included.
+ *    reaches not finite: infinities of one sign give it, others NaN.  The keys
+ *    past kv_len may hold anything, NaN included.
  *    B x max_kv_blocks (with tables: x groups) must be below 2^31.
  *    kv_len is taken as 0 below 0 and as 64 * max_kv_blocks above it; blocks
  *    whose table entry or page id is out of range add no keys.

@@ -206,7 +206,8 @@ __device__ __forceinline__ float2 get2(const float* p) {
 
 // Counts a piece of a row in; true for the last of n.  A counter is 0 between launches,
 // and each piece adds `piece`, a number of this launch with 1 in the low 16 bits: k pieces
-// are k * piece, which no other number of pieces of no other launch is.  A workspace may hold
+// are k * piece, which no number of pieces of another launch is (replays of one graph share
+// theirs).  A workspace may hold
 // anything at first, the counts of an earlier launch too whose pieces never came together:
 // who finds a value that is no count of this launch makes it one, with a swap that only
 // one of those who find it can win, and counts in if it is another.
