@@ -87,7 +87,7 @@
 extern "C" {
 #endif
 
-#define CA_ABI_VERSION 7
+#define CA_ABI_VERSION 8
 
 typedef enum ca_status {
   CA_OK = 0,
@@ -537,6 +537,128 @@ ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16
                               const int32_t* kv_indices, int32_t group_size, float sm_scale,
                               uint16_t* out, float* lse, void* ws, size_t ws_bytes,
                               void* stream);
+
+/* 5d. ca_rotary_append with norms: every head of q and k (before the turn) becomes
+ *        y_d = x_d / sqrt(mean_d(x_d^2) + eps) * w_d
+ *    over all of its head_dim elements, whatever rot_dim; w is q_weight or
+ *    k_weight, one [head_dim] for all heads, plus 1 with unit_offset.  A NULL weight
+ *    leaves that side without a norm.  Squares, their sum (in 32 bits: a head's mean
+ *    square must stay below 2^127), norm and turn are fp32, the result is
+ *    rounded once to bf16.  Values are not normalised.  Everything else is as in 5b.
+ * ---------------------------------------------------------------------- */
+typedef struct ca_head_norm {
+  const void* q_weight;       /* DEVICE [head_dim], 16-byte aligned; NULL: q as it is */
+  const void* k_weight;       /* DEVICE [head_dim], 16-byte aligned; NULL: k as it is */
+  int32_t weight_fp32;        /* 0: the weights are bf16; 1: fp32                     */
+  int32_t unit_offset;        /* 1: the weights are stored less 1                     */
+  float eps;                  /* finite, >= 0                                         */
+} ca_head_norm;
+
+ca_status ca_norm_rotary_append(const ca_cache* c, const ca_rotary* r, const ca_head_norm* n,
+                                int32_t num_tokens, const uint16_t* q, int64_t q_stride,
+                                const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                                int64_t v_stride, const int32_t* positions,
+                                const int64_t* slot_map, uint16_t* q_out, uint16_t* k_pool,
+                                uint16_t* v_pool, void* stream);
+
+/* ------------------------------------------------------------------------
+ * 6. Requests that share pages: several answers of one prompt, beams, requests
+ *    behind one system prompt.  page_shares int32 [num_pages] counts, for
+ *    every page, the requests that hold it besides the first: 0 for a page
+ *    that one request holds and for a free one.  ca_assign_slots needs
+ *    nothing of it (it gives out free pages); ca_release_pages knows nothing of
+ *    it, so requests that may share pages end by ca_fork_requests.
+ *    A page that several requests hold is full, so no one writes to it.
+ *
+ * 6a. ca_fork_requests: every row of the page table becomes a fork of a row as it was
+ *    before the call, or ends.  With r = parent[b] the request b afterwards has the
+ *    first n tokens of request r, n = seq_len[r], or min(seq_len[r],
+ *    max(keep_len[b], 0)) where keep_len is given; r outside 0 .. B - 1 ends
+ *    it (n = 0).  parent[b] = b and no keep_len leaves it as it is; rows that
+ *    go on from each other's (beams) are one call.
+ *      - whole pages (64 of the n tokens) are shared, page ids unchanged;
+ *      - a last page that n fills in part is taken over by one fork, if no one
+ *        else holds it: r itself, or the lowest b, where all other forks of r
+ *        end before it, row r has page_shares of 0 there for every head, and r no longer
+ *        holds more of it.  Every other fork gets a free page for each KV head (in
+ *        the order of the requests, then the heads, from the free list's end) and
+ *        the K and V pages are copied whole to it;
+ *      - where the free pages (as they were before the call) do not reach, a
+ *        request keeps its whole pages only: seq_len_out is then n - n % 64, as for
+ *        all requests after it that need a page;
+ *      - pages that no request holds any more go behind the free ones, by ascending id.
+ *    Lengths out of range (below 0, past max_kv_blocks) count as 0.  Entries that
+ *    are no page are handed on as they are, and a free page that is none is given away
+ *    but not written to.  free_capacity must be at least num_pages.
+ *    Written: seq_len_out [B], page_table_out (the blocks that the requests
+ *    then have; entries behind them are left alone), page_shares_out,
+ *    free_pages_out (the free ones) and free_count_out.  Each may be its input,
+ *    and a page table in place has only the rows that change written; other
+ *    buffers may not overlap.  The pools have the copies written.
+ *    Workspace: ca_fork_workspace_bytes(c) bytes, 16-byte aligned, whatever it
+ *    holds; calls that may overlap must not share one.
+ *
+ * 6b. ca_compact_pages: moves pages so that the U pages in use (all that are not in
+ *    the free list) have the ids below U: the i-th page in use from U on goes to
+ *    the i-th free id below U, both ascending; the others stay.  A smaller
+ *    pool, or the rest of it for something else, is then enough.
+ *    Written: new_page [num_pages] (where a page in use is now, -1 for a
+ *    free one), page_table_out (the blocks that the requests have, by seq_len; an
+ *    entry that is no page is handed on as it is), page_shares_out,
+ *    free_pages_out = num_pages - 1, .., U (so the lowest is taken first), free_count_out
+ *    = num_pages - U, and in the pools the pages that move (their old places keep
+ *    what they held).  Entries of the free list that are out of range or there
+ *    twice count once or not.  page_shares may be NULL, with page_shares_out.  Each output
+ *    but new_page may be its input.  free_capacity must be at least num_pages.
+ *    Workspace: ca_compact_workspace_bytes(c) bytes, as above.
+ * ---------------------------------------------------------------------- */
+size_t ca_fork_workspace_bytes(const ca_cache* c);
+
+ca_status ca_fork_requests(const ca_cache* c, const int32_t* parent, const int32_t* keep_len,
+                           const int32_t* seq_len, const int32_t* page_table,
+                           const int32_t* page_shares, const int32_t* free_pages,
+                           int32_t free_capacity, const int32_t* free_count, uint16_t* k_pool,
+                           uint16_t* v_pool, int32_t* seq_len_out, int32_t* page_table_out,
+                           int32_t* page_shares_out, int32_t* free_pages_out,
+                           int32_t* free_count_out, void* ws, size_t ws_bytes, void* stream);
+
+size_t ca_compact_workspace_bytes(const ca_cache* c);
+
+ca_status ca_compact_pages(const ca_cache* c, const int32_t* seq_len, const int32_t* page_table,
+                           const int32_t* page_shares, const int32_t* free_pages,
+                           int32_t free_capacity, const int32_t* free_count, uint16_t* k_pool,
+                           uint16_t* v_pool, int32_t* new_page, int32_t* page_table_out,
+                           int32_t* page_shares_out, int32_t* free_pages_out,
+                           int32_t* free_count_out, void* ws, size_t ws_bytes, void* stream);
+
+/* 6c. ca_decode_attention for requests that share prefixes, each read once for all
+ *    of its requests.  share int32 [B]: the share of request b, none where it is outside
+ *    0 .. num_shares - 1; share_len int32 [num_shares]: the tokens that the
+ *    requests of a share have in common, of which the whole pages count:
+ *    P = share_len / 64 (at most max_kv_blocks).  A request of the share with
+ *    kv_len >= 64 P is a member; one that is shorter (an idle row) is taken by itself.
+ *    The keys of blocks 0 .. P - 1 are read through the table row of the
+ *    share's first member, for all members, whose rows must name the same
+ *    pages there (as ca_fork_requests leaves them; if they do not, the first
+ *    member's count); the blocks behind, and everything of the others, through their own
+ *    rows.  A share with one member is read as if there were none.
+ *    q, out, lse, kv_len, sm_scale, empty requests, scores and values that are not finite and
+ *    what is out of range are as in 5c without tables; the softmax
+ *    weights meet v with 16 bits.  B <= 4096 and num_shares <= 1024 (else
+ *    CA_ERR_UNSUPPORTED); num_shares may be 0 (share and share_len are then not read).
+ *    B x max_kv_blocks x Hkv x ceil(Hq / Hkv / 256) must be below 2^31.
+ *    Workspace: ca_prefix_decode_workspace_bytes(c, num_shares) bytes (0 if
+ *    refused), 16-byte aligned, whatever it holds; calls that may overlap
+ *    must not share one.
+ * ---------------------------------------------------------------------- */
+size_t ca_prefix_decode_workspace_bytes(const ca_cache* c, int32_t num_shares);
+
+ca_status ca_prefix_decode_attention(const ca_cache* c, const uint16_t* q, const uint16_t* k_pool,
+                                     const uint16_t* v_pool, const int32_t* page_table,
+                                     const int32_t* kv_len, const int32_t* share,
+                                     const int32_t* share_len, int32_t num_shares, float sm_scale,
+                                     uint16_t* out, float* lse, void* ws, size_t ws_bytes,
+                                     void* stream);
 
 /* ------------------------------------------------------------------------
  * Debug helper: synchronises `stream`, copies the tables to the host and

@@ -34,7 +34,9 @@ EXPORTED = (
     "ca_select_blocks_threshold", "ca_estimate_masks_threshold", "ca_estimate_tables",
     "ca_build_block_tables_noalloc", "ca_check_tables_host",
     "ca_check_cache", "ca_assign_slots", "ca_release_pages", "ca_rotary_append",
-    "ca_decode_workspace_bytes", "ca_decode_attention",
+    "ca_decode_workspace_bytes", "ca_decode_attention", "ca_norm_rotary_append",
+    "ca_fork_workspace_bytes", "ca_fork_requests", "ca_compact_workspace_bytes",
+    "ca_compact_pages", "ca_prefix_decode_workspace_bytes", "ca_prefix_decode_attention",
 )
 
 
@@ -77,6 +79,16 @@ class CARotary(ctypes.Structure):
     ]
 
 
+class CAHeadNorm(ctypes.Structure):
+    _fields_ = [
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+        ("weight_fp32", ctypes.c_int32),
+        ("unit_offset", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+    ]
+
+
 # ca_problem.v_layout: V pages token-major [P, page, D] (the paper's layout, as
 # the K pages) or transposed [P, D, page]
 V_TOKEN_MAJOR = 0
@@ -107,7 +119,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     P = ctypes.POINTER(CAProblem)
     vp, i32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
     i64 = ctypes.c_int64
-    C, RO = ctypes.POINTER(CACache), ctypes.POINTER(CARotary)
+    C, RO, HN = ctypes.POINTER(CACache), ctypes.POINTER(CARotary), ctypes.POINTER(CAHeadNorm)
     sig = {
         "ca_abi_version": ([], ctypes.c_int),
         "ca_status_string": ([ctypes.c_int], ctypes.c_char_p),
@@ -147,9 +159,20 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
         "ca_release_pages": ([C, vp, vp, vp, vp, i32, vp, vp, vp, vp], ctypes.c_int),
         "ca_rotary_append": ([C, RO, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp],
                              ctypes.c_int),
+        "ca_norm_rotary_append": ([C, RO, HN, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp,
+                                   vp], ctypes.c_int),
         "ca_decode_workspace_bytes": ([C, i32], sz),
         "ca_decode_attention": ([C, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp],
                                 ctypes.c_int),
+        "ca_fork_workspace_bytes": ([C], sz),
+        "ca_fork_requests": ([C, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                              sz, vp], ctypes.c_int),
+        "ca_compact_workspace_bytes": ([C], sz),
+        "ca_compact_pages": ([C, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+                             ctypes.c_int),
+        "ca_prefix_decode_workspace_bytes": ([C, i32], sz),
+        "ca_prefix_decode_attention": ([C, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp],
+                                       ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -647,21 +670,43 @@ class Cache:
         self._v_pool = (num_pages, head_dim, page_size) if v_layout == V_TRANSPOSED else self._k_pool
 
 
+class HeadNorm:
+    """Norms of every head of queries and keys (ca_head_norm): x / sqrt(mean(x^2) + eps) * weight.
+
+    Weights bf16 or float32 ``[head_dim]`` on the GPU, both of one type (None: that side has no
+    norm); ``unit_offset``: they are stored less 1."""
+
+    def __init__(self, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
+                 eps: float = 1e-6, unit_offset: bool = False):
+        there = [w for w in (q_weight, k_weight) if w is not None]
+        if len({(w.dtype, w.shape, w.device) for w in there}) > 1:
+            raise ValueError("q_weight and k_weight must have one type, size and device")
+        if there and (there[0].dtype not in (torch.bfloat16, torch.float32) or there[0].dim() != 1):
+            raise ValueError("norm weights must be bfloat16 or float32 [head_dim]")
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.head_dim = there[0].numel() if there else None
+        self.device_index = there[0].get_device() if there else None
+        self.c = CAHeadNorm(_ptr(q_weight), _ptr(k_weight),
+                            int(bool(there) and there[0].dtype is torch.float32), int(unit_offset), eps)
+        self.ref = ctypes.byref(self.c)
+
+
 class Rotary:
     """How positions turn queries and keys (ca_rotary).
 
     ``inv_freq`` float32 ``[rot_dim / 2]`` on the GPU (None: no rotation);
     ``pair_axis``: the axis of every pair when positions have several (None:
-    all axis 0)."""
+    all axis 0); ``norm``: a HeadNorm that every head passes before it turns."""
 
     def __init__(self, inv_freq: Optional[torch.Tensor], interleaved: bool = False,
-                 num_axes: int = 1, pair_axis: Optional[Sequence[int]] = None):
+                 num_axes: int = 1, pair_axis: Optional[Sequence[int]] = None,
+                 norm: Optional[HeadNorm] = None):
         pairs = 0 if inv_freq is None else inv_freq.numel()
         if pairs and inv_freq.dtype != torch.float32:
             raise ValueError("inv_freq must be float32")
         if pair_axis is not None and len(pair_axis) != pairs:
             raise ValueError(f"pair_axis names {len(pair_axis)} axes for {pairs} pairs")
-        self.num_axes, self.inv_freq = num_axes, inv_freq
+        self.num_axes, self.inv_freq, self.norm = num_axes, inv_freq, norm
         self._axes = (ctypes.c_int32 * pairs)(*pair_axis) if pair_axis is not None else None
         self.c = CARotary(2 * pairs, int(interleaved), num_axes,
                           ctypes.cast(self._axes, _c_i32p) if self._axes is not None else None,
@@ -776,7 +821,8 @@ def rotary_append(c: Cache, r: Rotary, q: torch.Tensor, k: torch.Tensor, v: torc
                   stream=None) -> torch.Tensor:
     """Rotates q [T, Hq, D] and k [T, Hkv, D] by their positions ([T], or [axes, T]) and writes
     keys and values to slot_map's places in the pools; returns the rotated queries.  q, k and v
-    may be parts of one tensor (a token's heads together, tokens apart)."""
+    may be parts of one tensor (a token's heads together, tokens apart).  With ``r.norm`` the
+    heads of q and k are normalised first."""
     if stream is not None:
         return _on(stream, rotary_append, locals())
     index, st = _here(q)
@@ -790,13 +836,20 @@ def rotary_append(c: Cache, r: Rotary, q: torch.Tensor, k: torch.Tensor, v: torc
     place = (T,) if r.num_axes == 1 and positions.dim() == 1 else (r.num_axes, T)
     if r.inv_freq is not None and r.inv_freq.get_device() != index:
         raise ValueError(f"inv_freq on {r.inv_freq.device}, the tokens on cuda:{index}")
-    _check(load().ca_rotary_append(
-        c.ref, r.ref, T, qp, qs, kp, ks, vp, vs,
-        _need("positions", positions, torch.int32, place, index),
-        _need("slot_map", slot_map, torch.int64, (T, Hkv), index),
-        _need("out", out, bf, (T, Hq, D), index),
-        _need("k_pool", kv_pool[0], bf, c._k_pool, index),
-        _need("v_pool", kv_pool[1], bf, c._v_pool, index), st))
+    args = (T, qp, qs, kp, ks, vp, vs,
+            _need("positions", positions, torch.int32, place, index),
+            _need("slot_map", slot_map, torch.int64, (T, Hkv), index),
+            _need("out", out, bf, (T, Hq, D), index),
+            _need("k_pool", kv_pool[0], bf, c._k_pool, index),
+            _need("v_pool", kv_pool[1], bf, c._v_pool, index), st)
+    if r.norm is None:
+        _check(load().ca_rotary_append(c.ref, r.ref, *args))
+        return out
+    n = r.norm
+    if n.head_dim is not None and (n.head_dim != D or n.device_index != index):
+        raise ValueError(f"norm weights [{n.head_dim}] on device {n.device_index}, the heads have "
+                         f"{D} elements on cuda:{index}")
+    _check(load().ca_norm_rotary_append(c.ref, r.ref, n.ref, *args))
     return out
 
 

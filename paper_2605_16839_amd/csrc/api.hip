@@ -437,6 +437,104 @@ ca_status check_cache(const ca_cache* c, int32_t group_size, ca::CacheDims* d) {
   return ok();
 }
 
+ca_status need_workspace(const char* what, size_t need, const void* ws, size_t ws_bytes) {
+  if (ws == nullptr || ws_bytes < need)
+    return fail(CA_ERR_WORKSPACE, "%s needs %zu workspace bytes, got %zu", what, need,
+                ws == nullptr ? (size_t)0 : ws_bytes);
+  if (reinterpret_cast<uintptr_t>(ws) % 16 != 0)
+    return fail(CA_ERR_WORKSPACE, "workspace must be 16-byte aligned");
+  return ok();
+}
+
+// The cache of a call whose requests share prefixes.
+ca_status check_prefix(const ca_cache* c, int32_t num_shares, ca::CacheDims* d) {
+  const ca_status s = check_cache(c, 0, d);
+  if (s != CA_OK) return s;
+  if (num_shares < 0) return fail(CA_ERR_SHAPE, "num_shares must be >= 0");
+  if (d->B > ca::kPrefixRequests || num_shares > ca::kPrefixShares)
+    return fail(CA_ERR_UNSUPPORTED, "batch %d > %d, or num_shares %d > %d", d->B,
+                ca::kPrefixRequests, num_shares, ca::kPrefixShares);
+  const int tiles = (d->Hq / d->Hkv + ca::kPrefixRows - 1) / ca::kPrefixRows;
+  if ((long long)d->B * d->max_kv_blocks * d->Hkv * tiles > INT32_MAX)
+    return fail(CA_ERR_SHAPE, "the heads' blocks (batch x max_kv_blocks x num_kv_heads, x tiles of "
+                "%d heads) must be fewer than 2^31", ca::kPrefixRows);
+  return ok();
+}
+
+// n == nullptr: without norms.
+ca_status rotary_append(const ca_cache* c, const ca_rotary* r, const ca_head_norm* n,
+                        int32_t num_tokens, const uint16_t* q, int64_t q_stride,
+                        const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                        const int32_t* positions, const int64_t* slot_map, uint16_t* q_out,
+                        uint16_t* k_pool, uint16_t* v_pool, void* stream) {
+  ca::CacheDims d;
+  ca_status s = check_cache(c, 0, &d);
+  if (s != CA_OK) return s;
+  if (r == nullptr) return fail(CA_ERR_NULL, "rotary is NULL");
+  if (r->rot_dim < 0 || r->rot_dim > d.D || r->rot_dim % 16 != 0)
+    return fail(CA_ERR_UNSUPPORTED, "rot_dim %d is not a multiple of 16 in [0, %d]", r->rot_dim,
+                d.D);
+  if (r->num_axes < 1 || r->num_axes > 4)
+    return fail(CA_ERR_UNSUPPORTED, "num_axes %d not supported (1 to 4)", r->num_axes);
+  if (r->rot_dim > 0 && !r->inv_freq) return fail(CA_ERR_NULL, "inv_freq is required");
+  if (num_tokens < 0 || num_tokens > 1 << 23)
+    return fail(CA_ERR_SHAPE, "num_tokens %d out of range [0, 2^23]", num_tokens);
+  ca::AppendLaunch l = {};
+  if (n != nullptr) {
+    if (!(n->eps >= 0.f) || !std::isfinite(n->eps))
+      return fail(CA_ERR_SHAPE, "eps must be finite and >= 0, got %g", (double)n->eps);
+    if ((s = need_aligned16("q_weight and k_weight", n->q_weight, n->k_weight)) != CA_OK) return s;
+    l.norm = n->q_weight != nullptr || n->k_weight != nullptr;
+    l.q_weight = n->q_weight;
+    l.k_weight = n->k_weight;
+    l.weight_fp32 = n->weight_fp32 != 0;
+    l.weight_offset = n->unit_offset != 0 ? 1.f : 0.f;
+    l.eps = n->eps;
+  }
+  for (int i = 0; r->pair_axis_host && i < r->rot_dim / 2; ++i) {
+    const int axis = r->pair_axis_host[i];
+    if (axis < 0 || axis >= r->num_axes)
+      return fail(CA_ERR_SHAPE, "pair_axis_host[%d] = %d is not in [0, %d)", i, axis, r->num_axes);
+    l.pair_axis[i / 32] |= (uint64_t)axis << (2 * (i % 32));
+  }
+  const int64_t wq = (int64_t)d.Hq * d.D, wk = (int64_t)d.Hkv * d.D;
+  if (num_tokens > 1 && (q_stride < wq || k_stride < wk || v_stride < wk))
+    return fail(CA_ERR_SHAPE, "a token's stride is shorter than its heads");
+  if (q_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0)
+    return fail(CA_ERR_UNALIGNED, "token strides must be multiples of 8 elements");
+  if (num_tokens == 0) return ok();
+  if (!q || !k || !v || !positions || !slot_map || !q_out || !k_pool || !v_pool)
+    return fail(CA_ERR_NULL,
+                "q, k, v, positions, slot_map, q_out, k_pool and v_pool are required");
+  if ((s = need_aligned16("q, k, v, q_out, k_pool and v_pool", q, k, v, q_out, k_pool, v_pool)) !=
+      CA_OK)
+    return s;
+  if (reinterpret_cast<uintptr_t>(slot_map) % sizeof(int64_t) != 0)
+    return fail(CA_ERR_UNALIGNED, "slot_map must be 8-byte aligned");
+  // every work item reads the elements it writes, and only those: q_out may be
+  // q itself, token for token
+  if (q_out == q && q_stride != wq && num_tokens > 1)
+    return fail(CA_ERR_SHAPE, "q_out may be q only if q is dense");
+  l.q = q;
+  l.k = k;
+  l.v = v;
+  l.q_stride = q_stride;
+  l.k_stride = k_stride;
+  l.v_stride = v_stride;
+  l.positions = positions;
+  l.slot_map = slot_map;
+  l.inv_freq = r->inv_freq;
+  l.q_out = q_out;
+  l.k_pool = k_pool;
+  l.v_pool = v_pool;
+  l.num_tokens = num_tokens;
+  l.rot_dim = r->rot_dim;
+  l.num_axes = r->num_axes;
+  l.interleaved = r->interleaved != 0;
+  return hip_status(ca::launch_rotary_append(d, l, static_cast<hipStream_t>(stream)),
+                    "rotary append launch");
+}
+
 }  // namespace
 
 // Scratch of the allocation-free table builder: the union words and row counts
@@ -993,61 +1091,19 @@ ca_status ca_rotary_append(const ca_cache* c, const ca_rotary* r, int32_t num_to
                            int64_t k_stride, const uint16_t* v, int64_t v_stride,
                            const int32_t* positions, const int64_t* slot_map, uint16_t* q_out,
                            uint16_t* k_pool, uint16_t* v_pool, void* stream) {
-  ca::CacheDims d;
-  ca_status s = check_cache(c, 0, &d);
-  if (s != CA_OK) return s;
-  if (r == nullptr) return fail(CA_ERR_NULL, "rotary is NULL");
-  if (r->rot_dim < 0 || r->rot_dim > d.D || r->rot_dim % 16 != 0)
-    return fail(CA_ERR_UNSUPPORTED, "rot_dim %d is not a multiple of 16 in [0, %d]", r->rot_dim,
-                d.D);
-  if (r->num_axes < 1 || r->num_axes > 4)
-    return fail(CA_ERR_UNSUPPORTED, "num_axes %d not supported (1 to 4)", r->num_axes);
-  if (r->rot_dim > 0 && !r->inv_freq) return fail(CA_ERR_NULL, "inv_freq is required");
-  if (num_tokens < 0 || num_tokens > 1 << 23)
-    return fail(CA_ERR_SHAPE, "num_tokens %d out of range [0, 2^23]", num_tokens);
-  ca::AppendLaunch l = {};
-  for (int i = 0; r->pair_axis_host && i < r->rot_dim / 2; ++i) {
-    const int axis = r->pair_axis_host[i];
-    if (axis < 0 || axis >= r->num_axes)
-      return fail(CA_ERR_SHAPE, "pair_axis_host[%d] = %d is not in [0, %d)", i, axis, r->num_axes);
-    l.pair_axis[i / 32] |= (uint64_t)axis << (2 * (i % 32));
-  }
-  const int64_t wq = (int64_t)d.Hq * d.D, wk = (int64_t)d.Hkv * d.D;
-  if (num_tokens > 1 && (q_stride < wq || k_stride < wk || v_stride < wk))
-    return fail(CA_ERR_SHAPE, "a token's stride is shorter than its heads");
-  if (q_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0)
-    return fail(CA_ERR_UNALIGNED, "token strides must be multiples of 8 elements");
-  if (num_tokens == 0) return ok();
-  if (!q || !k || !v || !positions || !slot_map || !q_out || !k_pool || !v_pool)
-    return fail(CA_ERR_NULL,
-                "q, k, v, positions, slot_map, q_out, k_pool and v_pool are required");
-  if ((s = need_aligned16("q, k, v, q_out, k_pool and v_pool", q, k, v, q_out, k_pool, v_pool)) !=
-      CA_OK)
-    return s;
-  if (reinterpret_cast<uintptr_t>(slot_map) % sizeof(int64_t) != 0)
-    return fail(CA_ERR_UNALIGNED, "slot_map must be 8-byte aligned");
-  // every work item reads the elements it writes, and only those: q_out may be
-  // q itself, token for token
-  if (q_out == q && q_stride != wq && num_tokens > 1)
-    return fail(CA_ERR_SHAPE, "q_out may be q only if q is dense");
-  l.q = q;
-  l.k = k;
-  l.v = v;
-  l.q_stride = q_stride;
-  l.k_stride = k_stride;
-  l.v_stride = v_stride;
-  l.positions = positions;
-  l.slot_map = slot_map;
-  l.inv_freq = r->inv_freq;
-  l.q_out = q_out;
-  l.k_pool = k_pool;
-  l.v_pool = v_pool;
-  l.num_tokens = num_tokens;
-  l.rot_dim = r->rot_dim;
-  l.num_axes = r->num_axes;
-  l.interleaved = r->interleaved != 0;
-  return hip_status(ca::launch_rotary_append(d, l, static_cast<hipStream_t>(stream)),
-                    "rotary append launch");
+  return rotary_append(c, r, nullptr, num_tokens, q, q_stride, k, k_stride, v, v_stride, positions,
+                       slot_map, q_out, k_pool, v_pool, stream);
+}
+
+ca_status ca_norm_rotary_append(const ca_cache* c, const ca_rotary* r, const ca_head_norm* n,
+                                int32_t num_tokens, const uint16_t* q, int64_t q_stride,
+                                const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                                int64_t v_stride, const int32_t* positions,
+                                const int64_t* slot_map, uint16_t* q_out, uint16_t* k_pool,
+                                uint16_t* v_pool, void* stream) {
+  if (n == nullptr) return fail(CA_ERR_NULL, "norm is NULL");
+  return rotary_append(c, r, n, num_tokens, q, q_stride, k, k_stride, v, v_stride, positions,
+                       slot_map, q_out, k_pool, v_pool, stream);
 }
 
 size_t ca_decode_workspace_bytes(const ca_cache* c, int32_t group_size) {
@@ -1089,6 +1145,97 @@ ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16
                               lse, ws, gs, sm_scale};
   return hip_status(ca::launch_decode(d, l, static_cast<hipStream_t>(stream)),
                     "decode attention launch");
+}
+
+size_t ca_fork_workspace_bytes(const ca_cache* c) {
+  ca::CacheDims d;
+  return check_cache(c, 0, &d) == CA_OK ? ca::fork_ws_bytes(d) : 0;
+}
+
+ca_status ca_fork_requests(const ca_cache* c, const int32_t* parent, const int32_t* keep_len,
+                           const int32_t* seq_len, const int32_t* page_table,
+                           const int32_t* page_shares, const int32_t* free_pages,
+                           int32_t free_capacity, const int32_t* free_count, uint16_t* k_pool,
+                           uint16_t* v_pool, int32_t* seq_len_out, int32_t* page_table_out,
+                           int32_t* page_shares_out, int32_t* free_pages_out,
+                           int32_t* free_count_out, void* ws, size_t ws_bytes, void* stream) {
+  ca::CacheDims d;
+  ca_status s = check_cache(c, 0, &d);
+  if (s != CA_OK) return s;
+  if (!parent || !seq_len || !page_table || !page_shares || !free_pages || !free_count ||
+      !k_pool || !v_pool || !seq_len_out || !page_table_out || !page_shares_out ||
+      !free_pages_out || !free_count_out)
+    return fail(CA_ERR_NULL, "everything but keep_len is required");
+  if (free_capacity < d.num_pages)
+    return fail(CA_ERR_SHAPE, "free_capacity %d is less than num_pages %d", free_capacity,
+                d.num_pages);
+  if ((s = need_aligned16("k_pool and v_pool", k_pool, v_pool)) != CA_OK) return s;
+  if ((s = need_workspace("fork requests", ca::fork_ws_bytes(d), ws, ws_bytes)) != CA_OK) return s;
+  const ca::ForkLaunch l = {parent, keep_len, seq_len, page_table, page_shares, free_pages,
+                            free_count, k_pool, v_pool, seq_len_out, page_table_out,
+                            page_shares_out, free_pages_out, free_count_out, ws, free_capacity};
+  return hip_status(ca::launch_fork(d, l, static_cast<hipStream_t>(stream)), "fork requests launch");
+}
+
+size_t ca_compact_workspace_bytes(const ca_cache* c) {
+  ca::CacheDims d;
+  return check_cache(c, 0, &d) == CA_OK ? ca::compact_ws_bytes(d) : 0;
+}
+
+ca_status ca_compact_pages(const ca_cache* c, const int32_t* seq_len, const int32_t* page_table,
+                           const int32_t* page_shares, const int32_t* free_pages,
+                           int32_t free_capacity, const int32_t* free_count, uint16_t* k_pool,
+                           uint16_t* v_pool, int32_t* new_page, int32_t* page_table_out,
+                           int32_t* page_shares_out, int32_t* free_pages_out,
+                           int32_t* free_count_out, void* ws, size_t ws_bytes, void* stream) {
+  ca::CacheDims d;
+  ca_status s = check_cache(c, 0, &d);
+  if (s != CA_OK) return s;
+  if (!seq_len || !page_table || !free_pages || !free_count || !k_pool || !v_pool || !new_page ||
+      !page_table_out || !free_pages_out || !free_count_out)
+    return fail(CA_ERR_NULL, "everything but page_shares is required");
+  if ((page_shares == nullptr) != (page_shares_out == nullptr))
+    return fail(CA_ERR_NULL, "page_shares and page_shares_out come together");
+  if (free_capacity < d.num_pages)
+    return fail(CA_ERR_SHAPE, "free_capacity %d is less than num_pages %d", free_capacity,
+                d.num_pages);
+  if ((s = need_aligned16("k_pool and v_pool", k_pool, v_pool)) != CA_OK) return s;
+  if ((s = need_workspace("compact pages", ca::compact_ws_bytes(d), ws, ws_bytes)) != CA_OK)
+    return s;
+  const ca::CompactLaunch l = {seq_len, page_table, page_shares, free_pages, free_count, k_pool,
+                               v_pool, new_page, page_table_out, page_shares_out, free_pages_out,
+                               free_count_out, ws, free_capacity};
+  return hip_status(ca::launch_compact(d, l, static_cast<hipStream_t>(stream)),
+                    "compact pages launch");
+}
+
+size_t ca_prefix_decode_workspace_bytes(const ca_cache* c, int32_t num_shares) {
+  ca::CacheDims d;
+  return check_prefix(c, num_shares, &d) == CA_OK ? ca::prefix_ws_bytes(d) : 0;
+}
+
+ca_status ca_prefix_decode_attention(const ca_cache* c, const uint16_t* q, const uint16_t* k_pool,
+                                     const uint16_t* v_pool, const int32_t* page_table,
+                                     const int32_t* kv_len, const int32_t* share,
+                                     const int32_t* share_len, int32_t num_shares, float sm_scale,
+                                     uint16_t* out, float* lse, void* ws, size_t ws_bytes,
+                                     void* stream) {
+  ca::CacheDims d;
+  ca_status s = check_prefix(c, num_shares, &d);
+  if (s != CA_OK) return s;
+  if (!q || !k_pool || !v_pool || !page_table || !kv_len || !out)
+    return fail(CA_ERR_NULL, "q, k_pool, v_pool, page_table, kv_len and out are required");
+  if (num_shares > 0 && (!share || !share_len))
+    return fail(CA_ERR_NULL, "share and share_len are required");
+  if ((s = need_aligned16("q, k_pool, v_pool and out", q, k_pool, v_pool, out)) != CA_OK) return s;
+  if (!(sm_scale > 0.f) || !std::isfinite(sm_scale))
+    return fail(CA_ERR_SHAPE, "sm_scale must be finite and > 0, got %g", (double)sm_scale);
+  if ((s = need_workspace("prefix decode attention", ca::prefix_ws_bytes(d), ws, ws_bytes)) != CA_OK)
+    return s;
+  const ca::PrefixLaunch l = {q, k_pool, v_pool, page_table, kv_len, share, share_len, out, lse, ws,
+                              num_shares, sm_scale};
+  return hip_status(ca::launch_prefix(d, l, static_cast<hipStream_t>(stream)),
+                    "prefix decode attention launch");
 }
 
 }  // extern "C"

@@ -12,6 +12,8 @@
 // Transposed V pages want 64 tokens of a dimension side by side: tiles of 64 tokens
 // are turned over in LDS and leave in runs of 8 slots (4353 tokens: 38 us with
 // 2-byte stores, 20 with tiles).
+#include <type_traits>
+
 #include "common.hpp"
 #include "serving.hpp"
 
@@ -20,6 +22,7 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kMinTileTokens = 512;
+static_assert(kAppendThreads == 2 * 2 * kMaxPairs, "a thread for every weight");
 constexpr double kTurnsPerRadian = 0.15915494309189533576888;
 
 struct AppendArgs {
@@ -116,12 +119,28 @@ __device__ __forceinline__ void transposed_tile(const AppendArgs& a, int tile, T
   }
 }
 
+// Sum over the n = 4 or 8 lanes, side by side, that hold one head.
+__device__ __forceinline__ float head_sum(float x, int n) {
+  auto lane = [](float v, auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value,
+                                                      0xf, 0xf, true));
+  };
+  x += lane(x, std::integral_constant<int, 0xb1>{});    // quad_perm: lanes 1, 0, 3, 2
+  x += lane(x, std::integral_constant<int, 0x4e>{});    // 2, 3, 0, 1
+  const float other = lane(x, std::integral_constant<int, 0x141>{});   // 7 - lane, of every 8
+  return n == 8 ? x + other : x;
+}
+
 // The first v_tiles workgroups take tiles of values, the others a token each.
+// NORM: y = x * (sum x^2 / D + eps)^(-1/2) * w for every head first, over the 4 or 8
+// lanes that hold it, in fp32; nothing is rounded between norm and turn.
+template <bool NORM>
 __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const AppendArgs a) {
   __shared__ union {
     Tile tile;
     struct {
       float cos[kMaxPairs], sin[kMaxPairs];
+      float weight[2][2 * kMaxPairs];   // of queries and keys
     } turn;
   } s;
   if ((int)blockIdx.x < a.v_tiles) {
@@ -133,6 +152,14 @@ __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const App
   const AppendLaunch& l = a.l;
   const int tid = threadIdx.x, D = a.D, half = l.rot_dim / 2;
   const long long t = (int)blockIdx.x - a.v_tiles;
+  if constexpr (NORM) {
+    const int side = tid / (2 * kMaxPairs), d = tid % (2 * kMaxPairs);
+    const void* const from = side ? l.k_weight : l.q_weight;
+    if (from && d < D)
+      s.turn.weight[side][d] = l.weight_offset +
+          (l.weight_fp32 ? static_cast<const float*>(from)[d]
+                         : bf16_bits_to_float(static_cast<const uint16_t*>(from)[d]));
+  }
   if (tid < half) {
     const int axis = (int)(l.pair_axis[tid >> 5] >> (2 * (tid & 31))) & 3;
     const int pos = l.positions[(long long)axis * l.num_tokens + t];
@@ -166,6 +193,15 @@ __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const App
     float x[8], y[8];
     load8(src + o0, x);
     load8(src + o1, y);
+    if (NORM && (key ? l.k_weight : l.q_weight)) {
+      const float* const weight = s.turn.weight[key ? 1 : 0];
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += x[e] * x[e], sum += y[e] * y[e];
+      const float r = 1.f / sqrtf(head_sum(sum, per_head) / D + l.eps);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= r * weight[o0 + e], y[e] *= r * weight[o1 + e];
+    }
     if (c < turned) {
       if (l.interleaved) {
 #pragma unroll
@@ -221,7 +257,8 @@ hipError_t launch_rotary_append(const CacheDims& d, const AppendLaunch& l, hipSt
   // and 4.1, and 64 single tokens, an ordinary step, 4.9 and 5.5.
   const long long tiles = (long long)(l.num_tokens + kTileTokens - 1) / kTileTokens * d.Hkv * (d.D / kTileDims);
   if (a.v_transposed && l.num_tokens >= kMinTileTokens && tiles <= 1 << 22) a.v_tiles = (int)tiles;
-  rotary_append_kernel<<<a.v_tiles + l.num_tokens, kAppendThreads, 0, st>>>(a);
+  if (l.norm) rotary_append_kernel<true><<<a.v_tiles + l.num_tokens, kAppendThreads, 0, st>>>(a);
+  else rotary_append_kernel<false><<<a.v_tiles + l.num_tokens, kAppendThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 

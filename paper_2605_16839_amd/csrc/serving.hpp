@@ -1,5 +1,5 @@
 // Internal launcher interface of the serving step (slots, rotary append, decode
-// attention) between the C ABI (api.hip) and the kernels.
+// attention, requests that share pages) between the C ABI (api.hip) and the kernels.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -44,6 +44,11 @@ struct AppendLaunch {
   int num_tokens, rot_dim, num_axes;
   bool interleaved;
   uint64_t pair_axis[2];   // 2 bits per pair
+  // norms of the heads (norm): nullptr weights leave a side as it is
+  const void* q_weight;
+  const void* k_weight;
+  bool norm, weight_fp32;
+  float weight_offset, eps;
 };
 hipError_t launch_rotary_append(const CacheDims& d, const AppendLaunch& a, hipStream_t st);
 
@@ -63,5 +68,66 @@ struct DecodeLaunch {
 };
 size_t decode_ws_bytes(const CacheDims& d);
 hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& a, hipStream_t st);
+
+struct ForkLaunch {
+  const int32_t* parent;
+  const int32_t* keep_len;     // nullptr: all tokens
+  const int32_t* seq_len;
+  const int32_t* page_table;
+  const int32_t* page_shares;
+  const int32_t* free_pages;
+  const int32_t* free_count;
+  uint16_t* k_pool;
+  uint16_t* v_pool;
+  int32_t* seq_len_out;
+  int32_t* page_table_out;
+  int32_t* page_shares_out;
+  int32_t* free_pages_out;
+  int32_t* free_count_out;
+  void* ws;
+  int free_capacity;
+};
+size_t fork_ws_bytes(const CacheDims& d);
+hipError_t launch_fork(const CacheDims& d, const ForkLaunch& a, hipStream_t st);
+
+struct CompactLaunch {
+  const int32_t* seq_len;
+  const int32_t* page_table;
+  const int32_t* page_shares;  // nullptr: none
+  const int32_t* free_pages;
+  const int32_t* free_count;
+  uint16_t* k_pool;
+  uint16_t* v_pool;
+  int32_t* new_page;
+  int32_t* page_table_out;
+  int32_t* page_shares_out;
+  int32_t* free_pages_out;
+  int32_t* free_count_out;
+  void* ws;
+  int free_capacity;
+};
+size_t compact_ws_bytes(const CacheDims& d);
+hipError_t launch_compact(const CacheDims& d, const CompactLaunch& a, hipStream_t st);
+
+constexpr int kPrefixRequests = 4096;   // at most
+constexpr int kPrefixShares = 1024;
+constexpr int kPrefixRows = 256;        // query rows of a tile
+
+struct PrefixLaunch {
+  const uint16_t* q;
+  const uint16_t* k_pool;
+  const uint16_t* v_pool;
+  const int32_t* page_table;
+  const int32_t* kv_len;
+  const int32_t* share;
+  const int32_t* share_len;
+  uint16_t* out;
+  float* lse;
+  void* ws;
+  int num_shares;
+  float sm_scale;
+};
+size_t prefix_ws_bytes(const CacheDims& d);
+hipError_t launch_prefix(const CacheDims& d, const PrefixLaunch& a, hipStream_t st);
 
 }  // namespace ca
