@@ -35,6 +35,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "pages.hpp"
 #include "serving.hpp"
 
 namespace ca {
@@ -63,43 +64,17 @@ struct DecodeArgs {
   bool join_later;                  // decode_join_kernel joins the rows
 };
 
-template <typename T>
-__device__ __forceinline__ T uniform(T v) {
-  static_assert(sizeof(T) == 4, "");
-  return __builtin_bit_cast(T, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
-}
 __device__ __forceinline__ long long uniform64(long long v) {
   const unsigned lo = __builtin_amdgcn_readfirstlane((int)(unsigned)v);
   const int hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
   return (long long)(((unsigned long long)(unsigned)hi << 32) | lo);
 }
 
-__device__ __forceinline__ float max2(float a, float b) {
-  return __builtin_elementwise_maximum(a, b);   // a NaN stays
-}
-// Over the 4 lane groups that hold the same column.
-__device__ __forceinline__ float groups_max(float x) {
-  uint32_t u = __float_as_uint(x);
-  auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  u = __float_as_uint(max2(__uint_as_float(r[0]), __uint_as_float(r[1])));
-  r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float groups_sum(float x) {
-  uint32_t u = __float_as_uint(x);
-  auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  u = __float_as_uint(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-  r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 // The value of the lane 8 columns on.
 __device__ __forceinline__ float other_half(float x) {
   return __uint_as_float(
       __builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x128 /* row_ror:8 */, 0xf, 0xf, true));
 }
-
-// 2^x, and the maxima in log2 units: exp2 of -inf is 0.
-__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Pages of a workgroup's share at least.  A CU draws some 30 GB/s, so few pages go to
 // many: 2 to each for 1024 tokens of 8 KV heads take 10.2 us, 4 take 11.8 and 8 14.5 (1
@@ -159,34 +134,6 @@ __device__ __forceinline__ int item_pages(const DecodeArgs& a, int i) {
   const long long cap = (long long)a.items * a.max_kv_blocks;
   const long long n = (long long)end - at;
   return at < 0 || n < 0 || n > a.max_kv_blocks || end > cap ? 0 : (int)n;
-}
-
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-
-// Key that row r of 16-key tile kt of a page stands for: lane group g, which the
-// 16x16 result gives rows 4g .. 4g+3, then holds keys 32p + 8g .. 32p + 8g + 7
-// of the 32-key step p (tiles 2p, 2p + 1).
-constexpr int key_of(int kt, int r) {
-  return 32 * (kt >> 1) + 8 * (r >> 2) + 4 * (kt & 1) + (r & 3);
-}
-// Half a page in LDS: 32 keys of K or token-major V (rows of D), D / 2 rows of a
-// transposed V page (64 keys each).  16-byte chunk where chunk c of row r lies, so
-// that operand reads meet no bank twice:
-//   K: 16 lanes read 16 bytes each, of rows that differ in bits 0, 1, 3 and 4;
-//   token-major V: 32 lanes of a transpose read cover rows {0..3, 8..11} (+
-//     multiples) x 32 bytes, so bits 0, 1 and 3 pick the 32-byte pair;
-//   transposed V: 16 lanes read 16 bytes each, of 16 rows in a row.
-// Where rows are 128 bytes, two share the 256 bytes of all banks, by bit 0.
-enum Half { kHalfK, kHalfV, kHalfVT };
-template <int D, Half H>
-__device__ __forceinline__ int swizzle(int r, int c) {
-  if (H == kHalfVT) return c ^ ((r >> 1) & 7);
-  if (H == kHalfK)
-    return D == 128 ? (c ^ ((r & 3) | (((r >> 3) & 3) << 2)))
-                    : (c ^ (((r >> 1) & 1) | (((r >> 3) & 3) << 1)));
-  return D == 128 ? (c ^ (((r & 3) | (((r >> 3) & 1) << 2)) << 1))
-                  : (c ^ ((((r >> 1) & 1) | (((r >> 3) & 1) << 1)) << 1));
 }
 
 // What workgroups hand to each other goes past the XCD's L2, which the others do
