@@ -109,8 +109,8 @@ struct CompactLaunch {
 size_t compact_ws_bytes(const CacheDims& d);
 hipError_t launch_compact(const CacheDims& d, const CompactLaunch& a, hipStream_t st);
 
-constexpr int kPrefixRequests = 4096;   // at most
-constexpr int kPrefixShares = 1024;
+constexpr int kPrefixRequests = 2048;   // at most
+constexpr int kPrefixShares = 512;
 constexpr int kPrefixRows = 256;        // query rows of a tile
 
 struct PrefixLaunch {

@@ -146,11 +146,11 @@ def test_no_shares_is_decode_attention():
     assert ((a.float() - b.float()).abs() <= 2.1 * BF16_HALF * b.float().abs() + 2.0 ** -14).all()
 
 
-@pytest.mark.parametrize("B", [256, 1000, 4096])
+@pytest.mark.parametrize("B", [256, 1000, 2048])
 def test_many_requests(B):
     rng = np.random.default_rng(B)
-    share = rng.integers(-1, 1024 if B > 1000 else 30, B).tolist()
-    share_len = rng.integers(0, 200, 1024 if B > 1000 else 30).tolist()
+    share = rng.integers(-1, 512 if B > 1000 else 30, B).tolist()
+    share_len = rng.integers(0, 200, 512 if B > 1000 else 30).tolist()
     idle = rng.random(B) < 0.5
     lens = [0 if i else (0 if s < 0 else share_len[s]) + int(m) for s, m, i in zip(share, rng.integers(1, 70, B), idle)]
     _run(rng, share, share_len, lens, 2, 1, 64, 0)

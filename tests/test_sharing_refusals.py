@@ -63,7 +63,7 @@ def test_compact_refuses(lib, kw, code):
 @pytest.mark.parametrize("kw,code", [
     (dict(scale=0.0), "CA_ERR_SHAPE"), (dict(scale=float("nan")), "CA_ERR_SHAPE"),
     (dict(scale=float("inf")), "CA_ERR_SHAPE"), (dict(shares=-1), "CA_ERR_SHAPE"),
-    (dict(shares=1025), "CA_ERR_UNSUPPORTED"), (dict(q=FAKE + 8), "CA_ERR_UNALIGNED"),
+    (dict(shares=513), "CA_ERR_UNSUPPORTED"), (dict(q=FAKE + 8), "CA_ERR_UNALIGNED"),
     (dict(out=FAKE + 2), "CA_ERR_UNALIGNED"), (dict(k=FAKE + 8), "CA_ERR_UNALIGNED"),
     (dict(ws=None), "CA_ERR_WORKSPACE"), (dict(ws=FAKE + 8), "CA_ERR_WORKSPACE"),
     (dict(nbytes=8), "CA_ERR_WORKSPACE"), (dict(share=None), "CA_ERR_NULL"), (dict(share_len=None), "CA_ERR_NULL"),
@@ -76,11 +76,11 @@ def test_prefix_refuses(lib, kw, code):
 def test_prefix_refuses_sizes(lib):
     def status(**kw):
         return _call(lib, lib.ca_prefix_decode_attention, PREFIX, _cache(**kw).ref, ws=None)
-    assert status(batch=4097) == "CA_ERR_UNSUPPORTED" and status(batch=4096) == "CA_ERR_WORKSPACE"
-    assert status(batch=4096, max_kv_blocks=16384, num_q_heads=32, num_kv_heads=32) == "CA_ERR_SHAPE"
-    assert status(batch=4095, max_kv_blocks=16384, num_q_heads=32, num_kv_heads=32) == "CA_ERR_WORKSPACE"
-    assert status(batch=4095, max_kv_blocks=16384, num_q_heads=8 * 257, num_kv_heads=8) == "CA_ERR_WORKSPACE"
-    assert status(batch=4095, max_kv_blocks=16384, num_q_heads=32 * 257, num_kv_heads=32) == "CA_ERR_SHAPE"
+    assert status(batch=2049) == "CA_ERR_UNSUPPORTED" and status(batch=2048) == "CA_ERR_WORKSPACE"
+    assert status(batch=2048, max_kv_blocks=16384, num_q_heads=64, num_kv_heads=64) == "CA_ERR_SHAPE"
+    assert status(batch=2047, max_kv_blocks=16384, num_q_heads=64, num_kv_heads=64) == "CA_ERR_WORKSPACE"
+    assert status(batch=2047, max_kv_blocks=16384, num_q_heads=32 * 257, num_kv_heads=32) == "CA_ERR_WORKSPACE"
+    assert status(batch=2047, max_kv_blocks=16384, num_q_heads=64 * 257, num_kv_heads=64) == "CA_ERR_SHAPE"
 
 
 def test_null_and_bad_caches(lib):
@@ -91,7 +91,7 @@ def test_null_and_bad_caches(lib):
                           (lib.ca_prefix_decode_attention, PREFIX)):
             assert _call(lib, fn, names, c) in ("CA_ERR_NULL", "CA_ERR_UNSUPPORTED", "CA_ERR_SHAPE")
     assert lib.ca_prefix_decode_workspace_bytes(_cache().ref, -1) == 0
-    assert lib.ca_prefix_decode_workspace_bytes(_cache().ref, 1025) == 0
+    assert lib.ca_prefix_decode_workspace_bytes(_cache().ref, 513) == 0
     assert lib.ca_prefix_decode_workspace_bytes(_cache().ref, 0) > 0
 
 
