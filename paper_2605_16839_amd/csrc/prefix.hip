@@ -12,7 +12,16 @@
 //
 // S^T = K Q^T and O^T += V^T P^T are v_mfma_f32_16x16x32_bf16, as in the decode attention, but a page
 // is read from LDS by all waves, for 16 or 32 rows each.
+//
+// What bounds it (32 and 8 heads of 128): behind one prefix of 126976 tokens, 128 requests with up to 4096
+// of their own, 528 us, the softmax's VALU work: a page for 256 rows takes 3.4 us, of which MFMA 37% and LDS
+// 15%; 507 TFLOP/s.  Taking turns at MFMA and VALU between a SIMD's two waves, and scores a page ahead of
+// their weights, measured the same (534, 553), row sums by MFMA were slower (559).  Own pages and
+// short prefixes are bound by memory: 96 requests, 6 prefixes of 1500 to 16000 tokens, up to 6000 of their own,
+// 168 us, 4.4 TB/s.  The smallest calls, 15 us, are two launches and the walk from lengths to pages.
 #include <type_traits>
+
+#pragma clang diagnostic ignored "-Winline-asm"   // page_to_lds names m0, which is reserved, as what it changes
 
 #include "common.hpp"
 #include "pages.hpp"
@@ -64,10 +73,12 @@ __device__ __forceinline__ int rows_of_tile(long long rows) {
   const int tiles = tiles_of(rows);
   return tiles < 2 ? kTile : (int)(((rows + tiles - 1) / tiles + 31) / 32 * 32);
 }
-// What a page costs with so many rows to a tile, memory or MFMA and softmax, whichever takes longer.
+// What a page costs with so many rows to a tile, in units of which a page of up to 32 rows, that memory
+// bounds, has kCost.  Measured of a page: 1.2 us (8 rows), 1.5 (56), 2.2 (128), 3.4 (256).  These
+// costs against 4, 4, 6 and 7: 168 us and 188 for the 96 requests above, 528 and 537 for the 128.
 __device__ __forceinline__ int page_cost(long long rows) {
   const long long all = rows < kTile ? rows : rows_of_tile(rows);
-  return all <= 128 ? kCost : (all <= 192 ? 6 : 7);
+  return all <= 32 ? kCost : all <= 128 ? 5 : (all <= 192 ? 9 : 11);
 }
 
 // Where workgroup w's share begins on the line of costs, and the share of the page that begins at u.
@@ -95,15 +106,6 @@ __device__ __forceinline__ int share_blocks(const PrefixArgs& a, int s) {
   const int n = a.l.share_len[s] / kPage;
   return n < 0 ? 0 : (n < a.max_kv_blocks ? n : a.max_kv_blocks);
 }
-// The share that request b of len tokens is a member of, -1: none.
-__device__ __forceinline__ int share_of_request(const PrefixArgs& a, int b, int len) {
-  if (a.l.num_shares == 0) return -1;
-  const int s = a.l.share[b];
-  if (s < 0 || s >= a.l.num_shares) return -1;
-  const int blocks = share_blocks(a, s);
-  return blocks > 0 && len >= blocks * kPage ? s : -1;
-}
-
 struct Entry {          // a page of the stream
   int page, set, sub;   // sub: KV head and tile of the item
   int keys;             // its keys that count, 0: no page; kFirst, kLast: of its item; kStop: of the share
@@ -120,11 +122,12 @@ struct Shared {
   float2 merge_ml[4][2][16];
   Entry queue[kQueue + kRing];
   int start[kSets + 1];                // cost of the sets before a set
-  uint16_t count[kPrefixShares], first[kPrefixShares];   // members of a share, and the first
+  uint16_t blocks[kPrefixShares];      // whole pages of a share's prefix
+  uint16_t count[kPrefixShares], first[kPrefixShares];   // its members, and the first
   uint16_t share[kPrefixRequests];     // the share that a request is a member of, kNoShare
   uint16_t member[kTile + 2];          // requests of the tile at hand, in order
   int part[kWaves];
-  int pages_all, run_end;
+  int pages_all, kinds, run_end;
 };
 constexpr int kNoShare = 0xffff;
 
@@ -200,14 +203,14 @@ struct Line {
   __device__ __forceinline__ long long rows(int set) const { return (set < S ? s.count[set] : 1) * (long long)a.G; }
   // pages of one item of a set, items
   __device__ __forceinline__ int pages(int set) const {
-    if (set < S) return s.count[set] > 1 ? share_blocks(a, set) : 0;
+    if (set < S) return s.count[set] > 1 ? s.blocks[set] : 0;
     const int b = set - S, share = shared(b);
-    const int n = blocks_for(request_len(a, b)) - (share >= 0 ? share_blocks(a, share) : 0);
+    const int n = blocks_for(request_len(a, b)) - (share >= 0 ? s.blocks[share] : 0);
     return n > 0 ? n : 0;   // it is below 0 only if the lengths changed under the kernel
   }
   __device__ __forceinline__ int items(int set) const { return a.Hkv * (set < S ? tiles_of(rows(set)) : a.tiles); }
   __device__ __forceinline__ int cost(int set) const { return weighted ? page_cost(rows(set)) : 1; }
-  // whether a wave has all keys of a page for its 32 rows, or half of them for more than 128 rows to be too few
+  // whether a wave has all keys of a page for its 32 rows: more rows than four groups of 32; else two waves share one
   __device__ __forceinline__ bool all_keys(int set) const {
     const long long all = rows(set);
     return (all < kTile ? all : rows_of_tile(all)) > kTile / 2;
@@ -342,7 +345,7 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
     rows = (int)(every - (long long)tile * tile_rows);
     rows = rows < tile_rows ? rows : tile_rows;
     rg = MODE == kAllKeys ? wv : wv >> 1, kh = MODE == kAllKeys ? 0 : wv & 1;
-    active = 32 * rg < rows;
+    active = uniform(32 * rg < rows ? 1 : 0) != 0;   // a branch of the whole wave
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int r = 32 * rg + 16 * c + col;
@@ -548,7 +551,7 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
 #pragma unroll
     for (int c = 0; c < 2; ++c) store(ends, c, 32 * rg + 16 * c + col);
   };
-  // The pages from `from` to `to` on the line of costs, page by page: step(e, next, buf, first) for page e in
+  // The pages from `from` to `to` on the line of costs, page by page: step(e, next, buf, first, more) for page e in
   // place buf of the ring, the first of them or not.  Pairs: the last two waves ask for all pages, one for
   // K and one for V, so the others never wait for pages on their way when they wait for queries.
   auto stream = [&](auto ahead, auto step) __attribute__((always_inline)) {
@@ -608,7 +611,7 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
         for (int j = 0; j < R - 3; ++j) n_left += made_k[j] + made_v[j];
         vm_left(n_left);
         lds_barrier();
-        ask(i, ek, ev);
+        auto more = [&]() __attribute__((always_inline)) { ask(i, ek, ev); };
         if (VT && keys < kPage) {   // weights of 0 do not undo a NaN in V: columns behind the last key
           for (int at = 8 * tid; at < kPage * D; at += 8 * kThreads) {
             const int r = at / kPage, key = at % kPage;
@@ -629,7 +632,7 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
           next = s.queue[i + 1];
           next.set = uniform(next.set), next.sub = uniform(next.sub), next.keys = uniform(next.keys);
         }
-        step(e, next, buf, first);
+        step(e, next, buf, first, more);
         first = false;
       }
       ring = (ring + n) % R;
@@ -637,32 +640,18 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
     lds_barrier();
   };
 
-  if constexpr (MODE == kAllKeys) {
-    const bool late = wv >= kWaves / 2;   // one of the two waves of a SIMD
-    bool owes = false;   // the V^T P^T of the page before
+  if constexpr (MODE != kPair) {
+    constexpr std::integral_constant<int, MODE == kAllKeys ? 2 : 1> steps{};
     stream(begin,
-           [&](const Entry& e, const Entry&, int buf, bool first) __attribute__((always_inline)) {
-      const bool ends = (e.keys & (kLast | kStop)) != 0;
+           [&](const Entry& e, const Entry&, int buf, bool first, auto more) __attribute__((always_inline)) {
       if ((e.keys & kFirst) && !first) begin(e);
       if (active) {
-        // The late waves are half a page behind: their V^T P^T meets the others' scores and softmax, and
-        // theirs the others' V^T P^T, so that MFMA and VALU both have work.
-        if (owes) add_v(k2, k2, 0, (buf + R - 1) % R);
-        score(k2, k2, 0, buf, e.keys & 127);
-        weigh(k2, k2);
-        owes = late && !ends;
-        if (!owes) add_v(k2, k2, 0, buf);
-      }
-      if (ends) finish((e.keys & kLast) != 0, buf);
-    });
-  } else if constexpr (MODE == kHalfKeys) {
-    stream(begin,
-           [&](const Entry& e, const Entry&, int buf, bool first) __attribute__((always_inline)) {
-      if ((e.keys & kFirst) && !first) begin(e);
-      if (active) {
-        score(k1, k2, kh, buf, e.keys & 127);
-        weigh(k1, k2);
-        add_v(k1, k2, kh, buf);
+        score(steps, k2, kh, buf, e.keys & 127);
+        more();   // asked for while the weights are made
+        weigh(steps, k2);
+        add_v(steps, k2, kh, buf);
+      } else {
+        more();
       }
       if (e.keys & (kLast | kStop)) finish((e.keys & kLast) != 0, buf);
     });
@@ -678,7 +667,8 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
       store(waits_ends, 0, col);
     };
     stream([](const Entry&) {},
-           [&](const Entry& e, const Entry& next, int buf, bool first) __attribute__((always_inline)) {
+           [&](const Entry& e, const Entry& next, int buf, bool first, auto more) __attribute__((always_inline)) {
+      more();
       if (waits) end_pair();
       if (first || (e.keys & kFirst)) ++turn;
       if (wv >> 1 == turn % kPairs) {
@@ -716,13 +706,17 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(const PrefixArgs a)
   // ---- the stream, from the lengths -------------------------------------------
   int* const count = reinterpret_cast<int*>(&s.pages[0][0][0]);   // no page is there yet
   int* const first = count + kPrefixShares;
-  for (int i = tid; i < S; i += kThreads) count[i] = 0, first[i] = a.B;
-  if (tid == 0) s.pages_all = 0;
+  for (int i = tid; i < S; i += kThreads) count[i] = 0, first[i] = a.B, s.blocks[i] = (uint16_t)share_blocks(a, i);
+  if (tid == 0) s.pages_all = 0, s.kinds = 0;
   __syncthreads();
   for (int b = tid; b < a.B; b += kThreads) {
-    const int share = share_of_request(a, b, request_len(a, b));
-    s.share[b] = (uint16_t)(share < 0 ? kNoShare : share);
-    if (share >= 0) atomicAdd(&count[share], 1), atomicMin(&first[share], b);
+    const int len = request_len(a, b);
+    int share = S > 0 ? l.share[b] : -1;
+    if (share >= 0 && share < S && s.blocks[share] > 0 && len >= s.blocks[share] * kPage)
+      atomicAdd(&count[share], 1), atomicMin(&first[share], b);
+    else
+      share = kNoShare;
+    s.share[b] = (uint16_t)share;
   }
   __syncthreads();
   for (int i = tid; i < S; i += kThreads) s.count[i] = (uint16_t)count[i], s.first[i] = (uint16_t)first[i];
@@ -737,6 +731,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(const PrefixArgs a)
       const int n = line.pages(i) * line.items(i);
       s.start[i] = n;
       pages += n, cost += (double)n * page_cost(line.rows(i));
+      if (n > 0 && (i < S || a.G > kPairRows)) atomicOr(&s.kinds, line.all_keys(i) ? 2 : 1);
     }
     // by cost only where shares are long, and the line of costs is not
     if (pages > 0) atomicAdd(&s.pages_all, pages);
@@ -760,7 +755,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(const PrefixArgs a)
   const int u0 = share_start(total, w), u1 = share_start(total, w + 1);
 
   // ---- where the join finds the requests' parts: some requests each -------------
-  for (int b = w * kWaves + wv; b < a.B; b += kGroups * kWaves) {
+  for (int b = (kGroups - 1 - w) * kWaves + wv; b < a.B; b += kGroups * kWaves) {   // the last have least to do
     const int share = line.shared(b);
     int rank = 0;
     for (int i0 = 0; share >= 0 && i0 < b; i0 += kWave) {
@@ -781,13 +776,17 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(const PrefixArgs a)
   for (int u = u0, end = u1 < split ? u1 : split; u < end;) {
     const int set = line.set_at(u);
     const bool all_keys = uniform(line.all_keys(set) ? 1 : 0);
-    lds_barrier();
-    if (tid == 0) s.run_end = end;
-    lds_barrier();
-    for (int i = set + 1 + tid; i < sets; i += kThreads)
-      if (s.start[i] < s.start[i + 1] && s.start[i] < end && line.all_keys(i) != all_keys) atomicMin(&s.run_end, s.start[i]);
-    lds_barrier();
-    const int to = uniform(s.run_end);
+    int to = end;
+    if (s.kinds == 3) {   // up to the first set of the other kind
+      lds_barrier();
+      if (tid == 0) s.run_end = end;
+      lds_barrier();
+      for (int i = set + 1 + tid; i < sets; i += kThreads)
+        if (s.start[i] < s.start[i + 1] && s.start[i] < end && line.all_keys(i) != all_keys) atomicMin(&s.run_end, s.start[i]);
+      lds_barrier();
+      to = s.run_end;
+    }
+    to = uniform(to);
     if (all_keys) run_pages<D, VT, kAllKeys>(line, u, to);
     else run_pages<D, VT, kHalfKeys>(line, u, to);
     u = to;
