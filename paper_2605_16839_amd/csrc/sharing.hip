@@ -14,7 +14,11 @@
 // Compaction.  With U pages in use, the i-th used id from U on moves to the i-th free id
 // below U; both ranks are prefix sums over the ids.
 //
-// What bounds them: latency, launch by launch; with many pages to copy HBM, read and write.
+// What bounds them: latency, launch by launch; with many pages to copy HBM, read and write.  A prompt of
+// 32741 tokens (8 KV heads of 128) for 64 requests: 15.6 us a call, of which plan 4.2 (one workgroup, its
+// barriers), free 3.8, the rest the rows (four loads that wait for each other, then 504 pages copied); compaction
+// of a pool of 81K pages, half of them in use and 20K of those moved, 284 us, of which the moves 271: 1.33 GB
+// at 4.9 TB/s.
 #include "common.hpp"
 #include "serving.hpp"
 
@@ -24,6 +28,7 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kRowThreads = 256;
 constexpr int kChunks = 256;       // of the page ids
+constexpr int kMarks = 1024;       // entries of the free list that a workgroup takes together
 constexpr int kLdsRequests = 4096; // so many requests' marks lie in LDS
 
 struct Plan {
@@ -159,26 +164,34 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(const ForkArgs 
   }
 }
 
-// A whole page of each pool, to another place.
-__device__ __forceinline__ void copy_page(uint16_t* pool, int from, int to, int page_elems) {
-  const u32x4* src = reinterpret_cast<const u32x4*>(pool + (long long)from * page_elems);
-  u32x4* dst = reinterpret_cast<u32x4*>(pool + (long long)to * page_elems);
-  for (int i = threadIdx.x; i < page_elems / 8; i += kRowThreads) dst[i] = src[i];
+// A whole page of both pools, to another place: all loads before the first store, so that they wait together.
+// The pages differ.
+__device__ __forceinline__ void copy_pages(uint16_t* k_pool, uint16_t* v_pool, int from, int to, int page_elems) {
+  constexpr int N = kPage * 128 / 8 / kRowThreads;   // loads of a thread for a page of the largest heads
+  const long long src = (long long)from * page_elems, dst = (long long)to * page_elems;
+  u32x4 k[N], v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int at = 8 * (kRowThreads * i + (int)threadIdx.x);
+    if (at >= page_elems) continue;
+    k[i] = *reinterpret_cast<const u32x4*>(k_pool + src + at);
+    v[i] = *reinterpret_cast<const u32x4*>(v_pool + src + at);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int at = 8 * (kRowThreads * i + (int)threadIdx.x);
+    if (at >= page_elems) continue;
+    *reinterpret_cast<u32x4*>(k_pool + dst + at) = k[i];
+    *reinterpret_cast<u32x4*>(v_pool + dst + at) = v[i];
+  }
 }
 
-// blockIdx.x: the row, as a request (its new entries and copies) and as a parent (what
-// its pages gain and lose); blockIdx.y: some of the KV heads.
-__global__ __launch_bounds__(kRowThreads) void fork_rows_kernel(const ForkArgs a) {
+// What the row's pages gain and lose by its forks.
+__device__ __forceinline__ void fork_counts(const ForkArgs& a, int r, const Plan& me, int h0, int hs) {
   __shared__ int s_holds[1024];   // pages that each of the row's forks shares with it
   __shared__ int s_forks;
   const ForkLaunch& l = a.l;
-  const int tid = threadIdx.x, r = blockIdx.x;
-  const Plan me = a.plan[r];
-  const int h0 = blockIdx.y, hs = gridDim.y;
-  auto row_of = [&](int b, int h) { return ((long long)b * a.Hkv + h) * a.max_kv_blocks; };
-
-  // ---- what the row's pages gain and lose ----
-  const int old_blocks = blocks_for(me.old);
+  const int tid = threadIdx.x, old_blocks = blocks_for(me.old);
   for (int b0 = 0; b0 < a.B && old_blocks > 0; b0 += 1024) {
     __syncthreads();
     if (tid == 0) s_forks = 0;
@@ -195,34 +208,44 @@ __global__ __launch_bounds__(kRowThreads) void fork_rows_kernel(const ForkArgs a
     if (forks == 0 && lost == 0) continue;
     for (int h = h0; h < a.Hkv; h += hs)
       for (int j = tid; j < old_blocks; j += kRowThreads) {
+        const int page = l.page_table[((long long)r * a.Hkv + h) * a.max_kv_blocks + j];
         int gain = -lost;
+#pragma unroll 8
         for (int i = 0; i < forks; ++i) gain += s_holds[i] > j ? 1 : 0;
-        const int page = gain != 0 ? l.page_table[row_of(r, h) + j] : -1;
-        if (page < 0 || page >= a.num_pages) continue;
+        if (gain == 0 || page < 0 || page >= a.num_pages) continue;
         const int was = atomicAdd(l.page_shares_out + page, gain);
         const int freed = (was + gain < 0 ? 1 : 0) - (was < 0 ? 1 : 0);
         if (freed != 0) atomicAdd(a.chunk_freed + page / a.chunk, freed);
       }
   }
+}
 
-  // ---- its new entries ----
+// A request's new entries, and the copy of its last page.
+__device__ __forceinline__ void fork_entries(const ForkArgs& a, int r, const Plan& me, int h0, int hs) {
+  const ForkLaunch& l = a.l;
   if (me.src < 0 || (a.in_place && !changes(me, r))) return;
-  const int blocks = blocks_for(me.now), count = a.used[0];
+  const int tid = threadIdx.x, blocks = blocks_for(me.now), count = a.used[0];
   int32_t* const to = a.in_place ? a.stage : l.page_table_out;
   for (int h = h0; h < a.Hkv; h += hs) {
+    const long long mine = ((long long)r * a.Hkv + h) * a.max_kv_blocks;
+    const int32_t* const old = l.page_table + ((long long)me.src * a.Hkv + h) * a.max_kv_blocks;
     int fresh = -1;
-    if (me.fresh >= 0) fresh = l.free_pages[count - 1 - (me.fresh + h)];
-    for (int j = tid; j < blocks; j += kRowThreads)
-      to[row_of(r, h) + j] =
-          me.fresh >= 0 && j == blocks - 1 ? fresh : l.page_table[row_of(me.src, h) + j];
     if (me.fresh >= 0) {
-      const int from = l.page_table[row_of(me.src, h) + blocks - 1];
-      if (from >= 0 && from < a.num_pages && fresh >= 0 && fresh < a.num_pages && from != fresh) {
-        copy_page(l.k_pool, from, fresh, a.page_elems);
-        copy_page(l.v_pool, from, fresh, a.page_elems);
-      }
+      fresh = l.free_pages[count - 1 - (me.fresh + h)];
+      const int from = old[blocks - 1];
+      if (from >= 0 && from < a.num_pages && fresh >= 0 && fresh < a.num_pages && from != fresh)
+        copy_pages(l.k_pool, l.v_pool, from, fresh, a.page_elems);
     }
+    for (int j = tid; j < blocks; j += kRowThreads)
+      to[mine + j] = me.fresh >= 0 && j == blocks - 1 ? fresh : old[j];
   }
+}
+
+// blockIdx.x: the row, as a parent (blockIdx.z 0) or as a request (1); blockIdx.y: some of the KV heads.
+__global__ __launch_bounds__(kRowThreads) void fork_rows_kernel(const ForkArgs a) {
+  const Plan me = a.plan[blockIdx.x];
+  if (blockIdx.z == 0) fork_counts(a, blockIdx.x, me, blockIdx.y, gridDim.y);
+  else fork_entries(a, blockIdx.x, me, blockIdx.y, gridDim.y);
 }
 
 // Workgroup i: the pages of chunk i that have become free, its part of the free
@@ -285,14 +308,29 @@ __global__ __launch_bounds__(kRowThreads) void compact_clear_kernel(const Compac
   if (i0 < kChunks) a.chunk_free[i0] = 0;
 }
 
+// Counts of the chunks by way of LDS: with an atomic on a chunk's counter for every page, 41K free pages took
+// 29 us, most of it in line for the counters; so 5.
 __global__ __launch_bounds__(kRowThreads) void compact_mark_kernel(const CompactArgs a) {
-  const int n = free_count_of(a.l.free_count, a.l.free_capacity);
-  for (long long i = (long long)blockIdx.x * kRowThreads + threadIdx.x; i < n;
-       i += (long long)gridDim.x * kRowThreads) {
-    const int p = a.l.free_pages[i];
-    if (p >= 0 && p < a.num_pages && atomicExch(a.free + p, 1) == 0)
-      atomicAdd(a.chunk_free + p / a.chunk, 1);
+  __shared__ int s_count[kChunks];
+  const int n = free_count_of(a.l.free_count, a.l.free_capacity), tid = threadIdx.x;
+  constexpr int N = kMarks / kRowThreads;
+  s_count[tid] = 0;
+  __syncthreads();
+  for (long long i0 = (long long)blockIdx.x * kMarks; i0 < n; i0 += (long long)gridDim.x * kMarks) {
+    int p[N], was[N];
+#pragma unroll
+    for (int y = 0; y < N; ++y) {
+      const long long i = i0 + kRowThreads * y + tid;
+      p[y] = i < n ? a.l.free_pages[i] : -1;
+    }
+#pragma unroll
+    for (int y = 0; y < N; ++y) was[y] = p[y] >= 0 && p[y] < a.num_pages ? atomicExch(a.free + p[y], 1) : 1;
+#pragma unroll
+    for (int y = 0; y < N; ++y)
+      if (was[y] == 0) atomicAdd(&s_count[p[y] / a.chunk], 1);
   }
+  __syncthreads();
+  if (s_count[tid] > 0) atomicAdd(a.chunk_free + tid, s_count[tid]);
 }
 
 // Workgroup i: the ranks in chunk i.
@@ -363,10 +401,8 @@ __global__ __launch_bounds__(kRowThreads) void compact_move_kernel(const Compact
       l.page_table_out[row * a.max_kv_blocks + j] = p >= 0 && p < a.num_pages ? place(p) : p;
     }
   }
-  for (int i = blockIdx.x; i < moves; i += gridDim.x) {
-    copy_page(l.k_pool, a.from[i], a.to[i], a.page_elems);
-    copy_page(l.v_pool, a.from[i], a.to[i], a.page_elems);
-  }
+  for (int i = blockIdx.x; i < moves; i += gridDim.x)
+    copy_pages(l.k_pool, l.v_pool, a.from[i], a.to[i], a.page_elems);
   if (me == 0) l.free_count_out[0] = a.num_pages - U;
 }
 
@@ -404,7 +440,7 @@ hipError_t launch_fork(const CacheDims& d, const ForkLaunch& l, hipStream_t st) 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int heads = d.B >= 512 ? 1 : 512 / d.B;
-  fork_rows_kernel<<<dim3(d.B, heads < d.Hkv ? heads : d.Hkv), kRowThreads, 0, st>>>(a);
+  fork_rows_kernel<<<dim3(d.B, heads < d.Hkv ? heads : d.Hkv, 2), kRowThreads, 0, st>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   fork_free_kernel<<<kChunks, kRowThreads, 0, st>>>(a);
   return hipGetLastError();
@@ -425,7 +461,8 @@ hipError_t launch_compact(const CacheDims& d, const CompactLaunch& l, hipStream_
   compact_clear_kernel<<<grid, kRowThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  compact_mark_kernel<<<grid, kRowThreads, 0, st>>>(a);
+  const int marks = (d.num_pages + kMarks - 1) / kMarks;   // a grid-stride loop, and no free list is much longer
+  compact_mark_kernel<<<marks < 1024 ? marks : 1024, kRowThreads, 0, st>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   compact_rank_kernel<<<kChunks, kRowThreads, 0, st>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
