@@ -291,3 +291,20 @@ def test_binding_refuses():
         ca.sharing.fork_requests(c, i32(2), *state[:3], i32(8), i32(1), pools)
     with pytest.raises(ValueError, match="come together"):
         ca.sharing.compact_pages(c, state[0], state[1], None, state[3], state[4], pools, bufs=dict(page_shares=i32(9)))
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+def test_shares_of_all_sizes_in_one_call(layout):
+    """Few and many rows to a page one after another, tiles of more than 256 rows, pairs' own pages behind them;
+    from enough pages on that they are dealt by their cost, and more than a workgroup looks up together."""
+    rng = np.random.default_rng(13)
+    share = [0] * 3 + [1] * 40 + [2] * 2 + [3] * 20 + [-1] * 2 + [4] * 66
+    share_len = [700, 900, 64 * 30, 1300, 130]
+    order = rng.permutation(len(share))
+    share = [share[i] for i in order]
+    mine = rng.integers(0, 260, len(share)).tolist()
+    mine[3], mine[20] = 5000, 1
+    _run(rng, share, share_len, _behind(share, share_len, mine), 8, 2, 64, layout)
+    _run(rng, share, share_len, _behind(share, share_len, mine), 14, 1, 128, layout)
+    few = [0, 1, 0, -1, 1, 1, 0]
+    _run(rng, few, [64 * 700, 64 * 650], _behind(few, [64 * 700, 64 * 650], [1, 5000, 70, 30000, 64, 1, 0]), 40, 1, 64, layout)
