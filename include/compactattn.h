@@ -604,7 +604,8 @@ ca_status ca_norm_rotary_append(const ca_cache* c, const ca_rotary* r, const ca_
  *    pool, or the rest of it for something else, is then enough.
  *    Written: new_page [num_pages] (where a page in use is now, -1 for a
  *    free one), page_table_out (the blocks that the requests have, by seq_len; an
- *    entry that is no page is handed on as it is), page_shares_out,
+ *    entry that is no page is handed on as it is, one that names a free page
+ *    becomes -1), page_shares_out,
  *    free_pages_out = num_pages - 1, .., U (so the lowest is taken first), free_count_out
  *    = num_pages - U, and in the pools the pages that move (their old places keep
  *    what they held).  Entries of the free list that are out of range or there
@@ -644,7 +645,7 @@ ca_status ca_compact_pages(const ca_cache* c, const int32_t* seq_len, const int3
  *    rows.  A share with one member is read as if there were none.
  *    q, out, lse, kv_len, sm_scale, empty requests, scores and values that are not finite and
  *    what is out of range are as in 5c without tables; the softmax
- *    weights meet v with 16 bits.  B <= 2048 and num_shares <= 512 (else
+ *    weights meet v as two bf16 parts, 16 bits of them.  B <= 2048 and num_shares <= 512 (else
  *    CA_ERR_UNSUPPORTED); num_shares may be 0 (share and share_len are then not read).
  *    B x max_kv_blocks x Hkv x ceil(Hq / Hkv / 256) must be below 2^31.
  *    Workspace: ca_prefix_decode_workspace_bytes(c, num_shares) bytes (0 if

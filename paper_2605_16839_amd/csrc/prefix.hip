@@ -564,7 +564,7 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
       {
         const int span = line.weighted ? kThreads : kQueue;
         Entry e = {-1, -1, 0, 0};
-        if (tid < span && base + tid < to) e = look_up(base + tid, to);
+        if (tid < span && tid < to - base) e = look_up(base + tid, to);
         const unsigned long long hits = __ballot(e.set >= 0);
         if (lane == 0) s.part[wv] = __popcll(hits);
         lds_barrier();
@@ -574,7 +574,7 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
           n += s.part[v];
         }
         if (e.set >= 0) s.queue[at] = e;
-        base += span;
+        base = span < to - base ? base + span : to;
         lds_barrier();
       }
       // the loads of each of the steps before: K of the page R - 1 on, V of the page R - 2 on
