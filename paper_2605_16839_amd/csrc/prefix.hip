@@ -14,11 +14,12 @@
 // is read from LDS by all waves, for 16 or 32 rows each.
 //
 // What bounds it (32 and 8 heads of 128): behind one prefix of 126976 tokens, 128 requests with up to 4096
-// of their own, 528 us, the softmax's VALU work: a page for 256 rows takes 3.4 us, of which MFMA 37% and LDS
-// 15%; 507 TFLOP/s.  Taking turns at MFMA and VALU between a SIMD's two waves, and scores a page ahead of
-// their weights, measured the same (534, 553), row sums by MFMA were slower (559).  Own pages and
-// short prefixes are bound by memory: 96 requests, 6 prefixes of 1500 to 16000 tokens, up to 6000 of their own,
-// 168 us, 4.4 TB/s.  The smallest calls, 15 us, are two launches and the walk from lengths to pages.
+// of their own, 488 us, 549 TFLOP/s, the weights' VALU work: of a SIMD's cycles MFMA has 40% and VALU
+// instructions, with the exponentials' four rounds, about 70%; LDS 15%.  Taking turns at MFMA and VALU between a
+// SIMD's two waves, and scores a page ahead of their weights, measured the same, row sums by MFMA 6% more.
+// Own pages and short prefixes are bound by memory: 96 requests, 6 prefixes of 1500 to 16000 tokens,
+// up to 6000 of their own, 159 us, 4.65 TB/s.  The smallest calls, 15 us, are two launches and the walk from
+// lengths to pages.
 #include <type_traits>
 
 #pragma clang diagnostic ignored "-Winline-asm"   // page_to_lds names m0, which is reserved, as what it changes
@@ -75,7 +76,7 @@ __device__ __forceinline__ int rows_of_tile(long long rows) {
 }
 // What a page costs with so many rows to a tile, in units of which a page of up to 32 rows, that memory
 // bounds, has kCost.  Measured of a page: 1.2 us (8 rows), 1.5 (56), 2.2 (128), 3.4 (256).  These
-// costs against 4, 4, 6 and 7: 168 us and 188 for the 96 requests above, 528 and 537 for the 128.
+// costs against 4, 4, 6 and 7, a step before: 168 us and 188 for the 96 requests above, 528 and 537 for the 128.
 __device__ __forceinline__ int page_cost(long long rows) {
   const long long all = rows < kTile ? rows : rows_of_tile(rows);
   return all <= 32 ? kCost : all <= 128 ? 5 : (all <= 192 ? 9 : 11);
@@ -470,8 +471,9 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
     read_v(f[0], p0, buf);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      // weights to 16 bits, in two parts: the upper half of p's bits, and what that leaves, which is never
-      // negative, and never 0 so that an infinity of v stays one
+      // weights to 16 bits, in two parts: the upper half of p's bits, and what that leaves of p (1 + 2^-22), which
+      // is above 0 so that an infinity of v stays one (for a p from 2^-104 on; the 2^-22 is under the parts'
+      // own 2^-16).  The larger of the difference and 2^-126 took an instruction more: 495 us against 488
       u32x4 hi[NC], lo[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
@@ -480,9 +482,9 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
           const float u = x[2 * p + (e >> 1)][c][2 * (e & 1)], v = x[2 * p + (e >> 1)][c][2 * (e & 1) + 1];
           const uint32_t ub = __float_as_uint(u), vb = __float_as_uint(v);
           hi[c][e] = __builtin_amdgcn_perm(vb, ub, 0x07060302);
-          constexpr float kLeast = 0x1p-126f;
-          const f32x2 rest = {max2(u - __uint_as_float(ub & 0xffff0000u), kLeast),
-                              max2(v - __uint_as_float(vb & 0xffff0000u), kLeast)};
+          constexpr float kMore = 1.f + 0x1p-22f;
+          const f32x2 rest = {__builtin_fmaf(u, kMore, -__uint_as_float(ub & 0xffff0000u)),
+                              __builtin_fmaf(v, kMore, -__uint_as_float(vb & 0xffff0000u))};
           lo[c][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
         }
       if (p + 1 < NP) read_v(f[p + 1 < NP ? p + 1 : 0], p0 + p + 1, buf);
