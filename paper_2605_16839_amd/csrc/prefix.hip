@@ -14,11 +14,11 @@
 // is read from LDS by all waves, for 16 or 32 rows each.
 //
 // What bounds it (32 and 8 heads of 128): behind one prefix of 126976 tokens, 128 requests with up to 4096
-// of their own, 488 us, 549 TFLOP/s, the weights' VALU work: of a SIMD's cycles MFMA has 40% and VALU
+// of their own, 482 us, 556 TFLOP/s, the weights' VALU work: of a SIMD's cycles MFMA has 40% and VALU
 // instructions, with the exponentials' four rounds, about 70%; LDS 15%.  Taking turns at MFMA and VALU between a
 // SIMD's two waves, and scores a page ahead of their weights, measured the same, row sums by MFMA 6% more.
 // Own pages and short prefixes are bound by memory: 96 requests, 6 prefixes of 1500 to 16000 tokens,
-// up to 6000 of their own, 159 us, 4.65 TB/s.  The smallest calls, 15 us, are two launches and the walk from
+// up to 6000 of their own, 161 us, 4.6 TB/s.  The smallest calls, 15 us, are two launches and the walk from
 // lengths to pages.
 #include <type_traits>
 
@@ -97,6 +97,7 @@ __device__ __forceinline__ int share_of(int total, int u) {
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ int request_len(const PrefixArgs& a, int b) {
@@ -471,9 +472,8 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
     read_v(f[0], p0, buf);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      // weights to 16 bits, in two parts: the upper half of p's bits, and what that leaves of p (1 + 2^-22), which
-      // is above 0 so that an infinity of v stays one (for a p from 2^-104 on; the 2^-22 is under the parts'
-      // own 2^-16).  The larger of the difference and 2^-126 took an instruction more: 495 us against 488
+      // weights to 16 bits, in two parts: the upper half of p's bits, and what that leaves, which is never
+      // negative, and made no less than 2^-126 so that an infinity of v stays one
       u32x4 hi[NC], lo[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
@@ -482,10 +482,10 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
           const float u = x[2 * p + (e >> 1)][c][2 * (e & 1)], v = x[2 * p + (e >> 1)][c][2 * (e & 1) + 1];
           const uint32_t ub = __float_as_uint(u), vb = __float_as_uint(v);
           hi[c][e] = __builtin_amdgcn_perm(vb, ub, 0x07060302);
-          constexpr float kMore = 1.f + 0x1p-22f;
-          const f32x2 rest = {__builtin_fmaf(u, kMore, -__uint_as_float(ub & 0xffff0000u)),
-                              __builtin_fmaf(v, kMore, -__uint_as_float(vb & 0xffff0000u))};
-          lo[c][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
+          const f32x2 rest = {u - __uint_as_float(ub & 0xffff0000u), v - __uint_as_float(vb & 0xffff0000u)};
+          const u16x2 least = {0x80, 0x80};   // (bf16 that are not negative compare as integers)
+          lo[c][e] = __builtin_bit_cast(
+              uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, __builtin_convertvector(rest, bf16x2)), least));
         }
       if (p + 1 < NP) read_v(f[p + 1 < NP ? p + 1 : 0], p0 + p + 1, buf);
 #pragma unroll

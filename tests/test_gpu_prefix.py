@@ -308,3 +308,28 @@ def test_shares_of_all_sizes_in_one_call(layout):
     _run(rng, share, share_len, _behind(share, share_len, mine), 14, 1, 128, layout)
     few = [0, 1, 0, -1, 1, 1, 0]
     _run(rng, few, [64 * 700, 64 * 650], _behind(few, [64 * 700, 64 * 650], [1, 5000, 70, 30000, 64, 1, 0]), 40, 1, 64, layout)
+
+
+@pytest.mark.parametrize("far", [3, 20, 103, 104, 110, 112, 118, 125])
+def test_infinities_behind_small_weights(far):
+    """A weight of 2^-far, with no bits in its second part, still hands an infinity on, and only to its dimension."""
+    rng = np.random.default_rng(far)
+    share, share_len, lens = [0, 0, 0], [128], [200, 150, 131]
+    for layout, D, Hq in ((0, 64, 2), (1, 128, 100)):
+        kp, vp, table, rows, pages = _cache(rng, share, share_len, lens, 1, D, 4, poison=False)
+        kp[:] = 0
+        q = np.zeros((3, Hq, D), np.float32)
+        q[:, :, 0] = 1
+        for block, hit in ((1, [0, 1, 2]), (2, [1])):
+            b = hit[0] if block == 1 else 1
+            k, v = kp.copy(), vp.copy()
+            k[rows[b, 0, block], 2, 0] = synth.bf16_round(np.float32([-far]))[0]
+            v[rows[b, 0, block], 2, 7] = 0x7f80
+            c = ca.Cache(3, Hq, 1, D, 4, pages, v_layout=layout)
+            out, _ = ca.sharing.prefix_decode_attention(
+                c, bf16_dev(synth.bf16_round(q)), (bf16_dev(k), bf16_dev(v if layout == 0 else synth.v_pages_transposed(v))),
+                i32_dev(rows), i32_dev(lens), i32_dev(share), i32_dev(share_len), float(np.log(2.0)))
+            out = out.float().cpu().numpy()
+            want = np.zeros((3, Hq, D), bool)
+            want[hit, :, 7] = True
+            assert np.array_equal(np.isposinf(out), want) and np.isfinite(out[~want]).all()
