@@ -133,7 +133,8 @@ __device__ __forceinline__ float head_sum(float x, int n) {
 
 // The first v_tiles workgroups take tiles of values, the others a token each.
 // NORM: y = x * (sum x^2 / D + eps)^(-1/2) * w for every head first, over the 4 or 8
-// lanes that hold it, in fp32; nothing is rounded between norm and turn.
+// lanes that hold it, in fp32; nothing is rounded between norm and turn.  8192 tokens of 32 and 8
+// heads of 128 take 41.6 us with norms and 40 without, 202 MB at the rate of a copy either way.
 template <bool NORM>
 __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const AppendArgs a) {
   __shared__ union {

@@ -15,10 +15,10 @@
 // below U; both ranks are prefix sums over the ids.
 //
 // What bounds them: latency, launch by launch; with many pages to copy HBM, read and write.  A prompt of
-// 32741 tokens (8 KV heads of 128) for 64 requests: 15.6 us a call, of which plan 4.2 (one workgroup, its
-// barriers), free 3.8, the rest the rows (four loads that wait for each other, then 504 pages copied); compaction
-// of a pool of 81K pages, half of them in use and 20K of those moved, 284 us, of which the moves 271: 1.33 GB
-// at 4.9 TB/s.
+// 32741 tokens (8 KV heads of 128) for 64 requests: 15.9 us a call, of which plan 4.3 (one workgroup, its
+// barriers), rows 7.1 (four loads that wait for each other, then 504 pages copied), free 2.8; compaction
+// of a pool of 81K pages, half of them in use and 20K of those moved, 286 us, of which the moves 260: 1.33 GB
+// at 5 TB/s.
 #include "common.hpp"
 #include "serving.hpp"
 

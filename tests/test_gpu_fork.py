@@ -270,3 +270,17 @@ def test_calls_in_a_graph_and_on_a_stream():
         live = np.broadcast_to(np.arange(most) < -(-f["seq_len"] // 64)[:, None, None], (B, H, most))
         assert np.array_equal(packed["page_table"].cpu().numpy()[live], p["page_table"][live])
         assert int(packed["free_count"]) == len(p["free"])
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_more_rows_than_lds_holds(in_place):
+    """Marks of more than 4096 rows are in the workspace, and forks of one row are counted in several rounds."""
+    rng = np.random.default_rng(17)
+    B, most = 4200, 2
+    pages = 2 * B * most + 50
+    lens, table, shares, free = _state(rng, B, 1, most, pages, 2, 100)
+    parent = np.where(rng.random(B) < 0.6, 4150, rng.integers(-1, B, B))
+    lens[4150] = max(lens[4150], 1)
+    if table[4150, 0, 0] < 0:
+        table[4150, 0, 0] = free.pop()
+    _check_fork(rng, parent, rng.integers(0, 129, B), lens, table, shares, free, pages, 64, in_place)
