@@ -12,7 +12,7 @@
 // that have become free, in the order of their ids, and what is written in place.
 //
 // Compaction.  With U pages in use, the i-th used id from U on moves to the i-th free id
-// below U; both ranks are prefix sums over the ids.
+// below U; both ranks are prefix sums over the ids.  Small pools: FreeMap.
 //
 // What bounds them: latency, launch by launch; with many pages to copy HBM, read and write.  A prompt of
 // 32741 tokens (8 KV heads of 128) for 64 requests: 15.9 us a call, of which plan 4.3 (one workgroup, its
@@ -29,6 +29,7 @@ constexpr int kPlanThreads = 1024;
 constexpr int kRowThreads = 256;
 constexpr int kChunks = 256;       // of the page ids
 constexpr int kMarks = 1024;       // entries of the free list that a workgroup takes together
+constexpr int kLdsPages = 16384;   // a pool of so many is compacted by way of LDS
 constexpr int kLdsRequests = 4096; // so many requests' marks lie in LDS
 
 struct Plan {
@@ -165,21 +166,22 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(const ForkArgs 
 }
 
 // A whole page of both pools, to another place: all loads before the first store, so that they wait together.
-// The pages differ.
-__device__ __forceinline__ void copy_pages(uint16_t* k_pool, uint16_t* v_pool, int from, int to, int page_elems) {
+// The pages differ; thread: of kRowThreads.
+__device__ __forceinline__ void copy_pages(uint16_t* k_pool, uint16_t* v_pool, int from, int to, int page_elems,
+                                           int thread) {
   constexpr int N = kPage * 128 / 8 / kRowThreads;   // loads of a thread for a page of the largest heads
   const long long src = (long long)from * page_elems, dst = (long long)to * page_elems;
   u32x4 k[N], v[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int at = 8 * (kRowThreads * i + (int)threadIdx.x);
+    const int at = 8 * (kRowThreads * i + thread);
     if (at >= page_elems) continue;
     k[i] = *reinterpret_cast<const u32x4*>(k_pool + src + at);
     v[i] = *reinterpret_cast<const u32x4*>(v_pool + src + at);
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int at = 8 * (kRowThreads * i + (int)threadIdx.x);
+    const int at = 8 * (kRowThreads * i + thread);
     if (at >= page_elems) continue;
     *reinterpret_cast<u32x4*>(k_pool + dst + at) = k[i];
     *reinterpret_cast<u32x4*>(v_pool + dst + at) = v[i];
@@ -234,7 +236,7 @@ __device__ __forceinline__ void fork_entries(const ForkArgs& a, int r, const Pla
       fresh = l.free_pages[count - 1 - (me.fresh + h)];
       const int from = old[blocks - 1];
       if (from >= 0 && from < a.num_pages && fresh >= 0 && fresh < a.num_pages && from != fresh)
-        copy_pages(l.k_pool, l.v_pool, from, fresh, a.page_elems);
+        copy_pages(l.k_pool, l.v_pool, from, fresh, a.page_elems, tid);
     }
     for (int j = tid; j < blocks; j += kRowThreads)
       to[mine + j] = me.fresh >= 0 && j == blocks - 1 ? fresh : old[j];
@@ -295,6 +297,7 @@ __global__ __launch_bounds__(kRowThreads) void fork_free_kernel(const ForkArgs a
 struct CompactArgs {
   CompactLaunch l;
   int B, Hkv, max_kv_blocks, num_pages, page_elems, chunk;
+  bool apart;        // the free list and its count after the call are not those before it
   int* free;         // [num_pages]: 1 for a free page
   int* from;         // [num_pages / 2 + 1]: the pages that move, ascending, and
   int* to;           // where they go
@@ -402,8 +405,109 @@ __global__ __launch_bounds__(kRowThreads) void compact_move_kernel(const Compact
     }
   }
   for (int i = blockIdx.x; i < moves; i += gridDim.x)
-    copy_pages(l.k_pool, l.v_pool, a.from[i], a.to[i], a.page_elems);
+    copy_pages(l.k_pool, l.v_pool, a.from[i], a.to[i], a.page_elems, tid);
   if (me == 0) l.free_count_out[0] = a.num_pages - U;
+}
+
+// Pools of up to kLdsPages pages: every workgroup makes a map of the free ids in LDS, and takes its share
+// of everything; neither marks nor ranks go by way of memory, and one launch does what four do else, two in
+// place.  us so and with four, pages of 64 dimensions, half of them free: 300 pages 7.6 and 12.5, 4000 12.0 and
+// 20.4, 16384 25.7 and 34.3, 65536 (twice the workgroups) 137 and 128; nearly all free: 16384 12.4 and 16.8,
+// 65536 40 and 22, since every workgroup reads the whole free list.
+struct FreeMap {
+  uint32_t bits[kLdsPages / 32 + 1];   // 1: a free page
+  int before[kLdsPages / 32 + 1];      // free ids before a word
+  int words;
+
+  __device__ __forceinline__ bool free(int p) const { return (bits[p >> 5] >> (p & 31) & 1) != 0; }
+  __device__ __forceinline__ int free_below(int p) const {
+    return before[p >> 5] + __popc(bits[p >> 5] & ((1u << (p & 31)) - 1));
+  }
+  // the r-th id (from 0) that is free, or used; there is one
+  __device__ __forceinline__ int nth(int r, bool used) const {
+    int lo = 0, hi = words;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((used ? 32 * mid - before[mid] : before[mid]) <= r) lo = mid;
+      else hi = mid;
+    }
+    uint32_t left = used ? ~bits[lo] : bits[lo];
+    for (int i = used ? 32 * lo - before[lo] : before[lo]; i < r; ++i) left &= left - 1;
+    return 32 * lo + __ffs(left) - 1;
+  }
+};
+
+__device__ __forceinline__ void write_free_list(const CompactLaunch& l, int num_pages, int U, long long me, long long all) {
+  for (long long i = U + me; i < num_pages; i += all) l.free_pages_out[num_pages - 1 - i] = (int)i;
+  if (me == 0) l.free_count_out[0] = num_pages - U;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void compact_lds_kernel(const CompactArgs a) {
+  __shared__ FreeMap s_map;
+  __shared__ int s_part[kPlanThreads / kWave];
+  __shared__ int s_from[kPlanThreads], s_to[kPlanThreads];   // of the moves at hand
+  const CompactLaunch& l = a.l;
+  const int tid = threadIdx.x, words = (a.num_pages + 31) / 32;
+  const long long all = (long long)gridDim.x * kPlanThreads, me = (long long)blockIdx.x * kPlanThreads + tid;
+  if (tid == 0) s_map.words = words;
+  if (tid <= words) s_map.bits[tid] = 0;
+  __syncthreads();
+  const int n = free_count_of(l.free_count, l.free_capacity);
+#pragma unroll 4
+  for (int i = tid; i < n; i += kPlanThreads) {
+    const int p = l.free_pages[i];
+    if (p >= 0 && p < a.num_pages) atomicOr(&s_map.bits[p >> 5], 1u << (p & 31));
+  }
+  __syncthreads();
+  static_assert(kLdsPages / 32 < kPlanThreads, "a thread for every word, and one behind");
+  const int mine = tid <= words ? __popc(s_map.bits[tid]) : 0;
+  int total;
+  const int upto = block_sum(mine, s_part, &total);
+  if (tid <= words) s_map.before[tid] = upto - mine;
+  __syncthreads();
+  const int U = a.num_pages - total, moves = s_map.free_below(U);
+  auto place = [&](int p) {
+    if (s_map.free(p)) return -1;
+    return p < U ? p : s_map.nth(p - s_map.free_below(p) - (U - moves), false);
+  };
+  for (long long i = me; i < a.num_pages; i += all) {
+    const int p = (int)i, at = place(p);
+    l.new_page[p] = at;
+    if (l.page_shares) {
+      if (at >= 0) {
+        const int holds = l.page_shares[p];
+        l.page_shares_out[at] = holds;
+      }
+      if (p >= U) l.page_shares_out[p] = 0;
+    }
+  }
+  const long long rows = (long long)a.B * a.Hkv;
+  for (long long row = (long long)blockIdx.x * (kPlanThreads / kWave) + (tid >> 6); row < rows;
+       row += (long long)gridDim.x * (kPlanThreads / kWave)) {
+    const int blocks = blocks_for(length_of(l.seq_len[row / a.Hkv], a.max_kv_blocks));
+    for (int j = tid & 63; j < blocks; j += kWave) {
+      const int p = l.page_table[row * a.max_kv_blocks + j];
+      l.page_table_out[row * a.max_kv_blocks + j] = p >= 0 && p < a.num_pages ? place(p) : p;
+    }
+  }
+  if (a.apart) write_free_list(l, a.num_pages, U, me, all);   // else others may still read it
+  else if (me == 0) a.count[0] = U;
+  // move i: the i-th id in use from U on to the i-th free one
+  const int first = (int)((long long)moves * blockIdx.x / gridDim.x);
+  const int last = (int)((long long)moves * (blockIdx.x + 1) / gridDim.x);
+  for (int i0 = first; i0 < last; i0 += kPlanThreads) {
+    const int some = last - i0 < kPlanThreads ? last - i0 : kPlanThreads;
+    __syncthreads();
+    if (tid < some) s_from[tid] = s_map.nth(U - moves + i0 + tid, true), s_to[tid] = s_map.nth(i0 + tid, false);
+    __syncthreads();
+    for (int i = tid / kRowThreads; i < some; i += kPlanThreads / kRowThreads)
+      copy_pages(l.k_pool, l.v_pool, s_from[i], s_to[i], a.page_elems, tid % kRowThreads);
+  }
+}
+
+__global__ __launch_bounds__(kRowThreads) void compact_list_kernel(const CompactArgs a) {
+  write_free_list(a.l, a.num_pages, a.count[0], (long long)blockIdx.x * kRowThreads + threadIdx.x,
+                  (long long)gridDim.x * kRowThreads);
 }
 
 int chunk_of(int num_pages) {   // ids of a chunk: whole rounds of a workgroup's threads
@@ -451,13 +555,22 @@ size_t compact_ws_bytes(const CacheDims& d) {
 }
 
 hipError_t launch_compact(const CacheDims& d, const CompactLaunch& l, hipStream_t st) {
-  CompactArgs a = {l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, kPage * d.D, chunk_of(d.num_pages)};
+  CompactArgs a = {l, d.B, d.Hkv, d.max_kv_blocks, d.num_pages, kPage * d.D, chunk_of(d.num_pages),
+                   l.free_pages_out != l.free_pages && l.free_count_out != l.free_count};
   a.free = static_cast<int*>(l.ws);
   a.from = a.free + d.num_pages;
   a.to = a.from + (d.num_pages / 2 + 1);
   a.chunk_free = a.to + (d.num_pages / 2 + 1);
   a.count = a.chunk_free + kChunks;
   const int each = (d.num_pages + kRowThreads - 1) / kRowThreads, grid = each < 1024 ? each : 1024;
+  if (d.num_pages <= kLdsPages) {
+    const int wanted = d.num_pages / 16 + 1;   // half of the pages move at most, four at a time
+    compact_lds_kernel<<<wanted < 256 ? wanted : 256, kPlanThreads, 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.apart) return e;
+    compact_list_kernel<<<grid, kRowThreads, 0, st>>>(a);
+    return hipGetLastError();
+  }
   compact_clear_kernel<<<grid, kRowThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

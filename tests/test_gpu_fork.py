@@ -284,3 +284,10 @@ def test_more_rows_than_lds_holds(in_place):
     if table[4150, 0, 0] < 0:
         table[4150, 0, 0] = free.pop()
     _check_fork(rng, parent, rng.integers(0, 129, B), lens, table, shares, free, pages, 64, in_place)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("pages", [31, 32, 33, 1024, 8160, 16351, 16383, 16384, 16385])
+def test_compact_of_small_and_larger_pools(pages, in_place):
+    """Sizes at which the last word of a map in LDS ends, and on both sides of the largest pool with one."""
+    test_compact(4, 2 if pages > 40 else 1, 2 if pages < 40 else 20, pages, True, 64, in_place)
