@@ -645,7 +645,8 @@ ca_status ca_compact_pages(const ca_cache* c, const int32_t* seq_len, const int3
  *    rows.  A share with one member is read as if there were none.
  *    q, out, lse, kv_len, sm_scale, empty requests, scores and values that are not finite and
  *    what is out of range are as in 5c without tables; the softmax
- *    weights meet v as two bf16 parts, 16 bits of them.  B <= 2048 and num_shares <= 512 (else
+ *    weights meet v as two bf16 parts, 16 bits of them, a weight that is not 0 with
+ *    2^-126 more at most (relative to the row's largest, as all of them are).  B <= 2048 and num_shares <= 512 (else
  *    CA_ERR_UNSUPPORTED); num_shares may be 0 (share and share_len are then not read).
  *    B x max_kv_blocks x Hkv x ceil(Hq / Hkv / 256) must be below 2^31.
  *    Workspace: ca_prefix_decode_workspace_bytes(c, num_shares) bytes (0 if

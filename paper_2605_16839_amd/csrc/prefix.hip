@@ -473,7 +473,8 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       // weights to 16 bits, in two parts: the upper half of p's bits, and what that leaves, which is never
-      // negative, and made no less than 2^-126 so that an infinity of v stays one
+      // negative.  The second part of a weight that is not 0 is made no less than 2^-126, so that an infinity of v stays
+      // one; a weight of 0 has none, and adds nothing however large v is.
       u32x4 hi[NC], lo[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
@@ -481,9 +482,11 @@ __device__ __forceinline__ void run_pages(const Line<D>& line, int from, int to)
         for (int e = 0; e < 4; ++e) {
           const float u = x[2 * p + (e >> 1)][c][2 * (e & 1)], v = x[2 * p + (e >> 1)][c][2 * (e & 1) + 1];
           const uint32_t ub = __float_as_uint(u), vb = __float_as_uint(v);
-          hi[c][e] = __builtin_amdgcn_perm(vb, ub, 0x07060302);
+          const uint32_t first = __builtin_amdgcn_perm(vb, ub, 0x07060302);
+          hi[c][e] = first;   // (__builtin_bit_cast of hi[c][e] itself would take hi[c][0])
           const f32x2 rest = {u - __uint_as_float(ub & 0xffff0000u), v - __uint_as_float(vb & 0xffff0000u)};
-          const u16x2 least = {0x80, 0x80};   // (bf16 that are not negative compare as integers)
+          // (bf16 that are not negative compare as integers)
+          const u16x2 least = __builtin_elementwise_min(__builtin_bit_cast(u16x2, first), u16x2{0x80, 0x80});
           lo[c][e] = __builtin_bit_cast(
               uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, __builtin_convertvector(rest, bf16x2)), least));
         }

@@ -333,3 +333,43 @@ def test_infinities_behind_small_weights(far):
             want = np.zeros((3, Hq, D), bool)
             want[hit, :, 7] = True
             assert np.array_equal(np.isposinf(out), want) and np.isfinite(out[~want]).all()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("D,Hq,members", [(64, 2, 3), (128, 4, 2), (128, 40, 2), (64, 100, 3), (128, 12, 20)])
+def test_keys_without_weight_add_nothing(D, Hq, members, layout):
+    """Scores of -inf, and scores so far below the largest that the weight is 0, meet values near the largest bf16:
+    half of the prefix's keys and of each request's own."""
+    rng = np.random.default_rng(D + Hq)
+    share, share_len = [0] * members, [128]
+    lens = [128 + int(n) for n in rng.integers(60, 100, members)]
+    kp, vp, table, rows, pages = _cache(rng, share, share_len, lens, 1, D, 4, poison=False)
+    q = np.zeros((members, Hq, D), np.float32)
+    q[:, :, 0] = 1
+    far = rng.random((pages, 64)) < 0.5
+    vp[far] = synth.bf16_round(rng.choice(np.float32([3.3e38, -3.3e38]), (int(far.sum()), D)))
+    for b in range(members):
+        far[rows[b, 0, [0, 2]], 3] = False          # every request keeps a key of either kind
+    for score in (0xff80, synth.bf16_round(np.float32([-300]))[0], synth.bf16_round(np.float32([-3e38]))[0]):
+        k = np.zeros_like(kp)
+        k[far, 0] = score
+        v = vp.copy()
+        v[~far & (np.abs(synth.bf16_bits_to_f32(vp[:, :, 0])) > 1e30)] = 0
+        c = ca.Cache(members, Hq, 1, D, 4, pages, v_layout=layout)
+        lse = torch.full((members, Hq), 7.0, device=DEV)
+        out, _ = ca.sharing.prefix_decode_attention(
+            c, bf16_dev(synth.bf16_round(q)), (bf16_dev(k), bf16_dev(v if layout == 0 else synth.v_pages_transposed(v))),
+            i32_dev(rows), i32_dev(lens), i32_dev(share), i32_dev(share_len), float(np.log(2.0)), lse=lse)
+        torch.cuda.synchronize()
+        # the definition over the keys that have a weight: all have the score 0, so the mean of their values
+        # (2^-300 of a value is below 2^-172).  Weights are 1 exactly, or 2^-8 at least where the maximum lags; their
+        # sums take 2^-19 of the mass, as above.
+        for b in range(members):
+            n = lens[b]
+            ids = rows[b, 0, np.arange(n) // 64]
+            there = ~far[ids, np.arange(n) % 64]
+            vals = synth.bf16_bits_to_f32(v[ids, np.arange(n) % 64]).astype(np.float64)[there]
+            want, mass = vals.mean(0), np.abs(vals).mean(0)
+            err = np.abs(bf16_host_f64(out[b]) - want)
+            assert (err <= BF16_HALF * np.abs(want) + (2.0 ** -16 + 2.0 ** -19) * mass).all(), (score, b, err.max())
+            assert np.abs(lse[b].cpu().numpy() - np.log(there.sum())).max() <= 2.0 ** -19 * np.log(there.sum())
