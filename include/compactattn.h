@@ -542,9 +542,10 @@ ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16
  *        y_d = x_d / sqrt(mean_d(x_d^2) + eps) * w_d
  *    over all of its head_dim elements, whatever rot_dim; w is q_weight or
  *    k_weight, one [head_dim] for all heads, plus 1 with unit_offset.  A NULL weight
- *    leaves that side without a norm.  Squares, their sum (in 32 bits: a head's mean
- *    square must stay below 2^127), norm and turn are fp32, the result is
- *    rounded once to bf16.  Values are not normalised.  Everything else is as in 5b.
+ *    leaves that side without a norm.  Squares, their sum, norm and turn are fp32, heads of
+ *    any size are in range (w below 2^100), and the result is rounded once to bf16.  With eps = 0 a head of zeros becomes NaN, with
+ *    any eps one that holds an infinity NaN there and 0 elsewhere, one that holds a NaN NaN.
+ *    Values are not normalised.  Everything else is as in 5b.
  * ---------------------------------------------------------------------- */
 typedef struct ca_head_norm {
   const void* q_weight;       /* DEVICE [head_dim], 16-byte aligned; NULL: q as it is */

@@ -12,6 +12,7 @@
 // Transposed V pages want 64 tokens of a dimension side by side: tiles of 64 tokens
 // are turned over in LDS and leave in runs of 8 slots (4353 tokens: 38 us with
 // 2-byte stores, 20 with tiles).
+#include <cmath>
 #include <type_traits>
 
 #include "common.hpp"
@@ -31,6 +32,7 @@ struct AppendArgs {
   long long num_slots;
   bool v_transposed;
   int v_tiles;
+  float root_eps;
 };
 
 __device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
@@ -119,21 +121,36 @@ __device__ __forceinline__ void transposed_tile(const AppendArgs& a, int tile, T
   }
 }
 
-// Sum over the n = 4 or 8 lanes, side by side, that hold one head.
-__device__ __forceinline__ float head_sum(float x, int n) {
+// The product that rounds by itself is named: which one the compiler fuses changes with what is around it.
+__device__ __forceinline__ void turn(float p, float q, float cs, float sn, float& x, float& y) {
+  x = __builtin_fmaf(p, cs, -(q * sn));
+  y = __builtin_fmaf(q, cs, p * sn);
+}
+
+// x of the n = 4 or 8 lanes, side by side, that hold one head, taken together.
+template <typename Op>
+__device__ __forceinline__ float over_head(float x, int n, Op op) {
   auto lane = [](float v, auto ctrl) {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value,
                                                       0xf, 0xf, true));
   };
-  x += lane(x, std::integral_constant<int, 0xb1>{});    // quad_perm: lanes 1, 0, 3, 2
-  x += lane(x, std::integral_constant<int, 0x4e>{});    // 2, 3, 0, 1
+  x = op(x, lane(x, std::integral_constant<int, 0xb1>{}));    // quad_perm: lanes 1, 0, 3, 2
+  x = op(x, lane(x, std::integral_constant<int, 0x4e>{}));    // 2, 3, 0, 1
   const float other = lane(x, std::integral_constant<int, 0x141>{});   // 7 - lane, of every 8
-  return n == 8 ? x + other : x;
+  return n == 8 ? op(x, other) : x;
+}
+
+// The power of two that brings x >= 0 to [1, 2), where both are normal.
+__device__ __forceinline__ float to_one(float x) {
+  const int e = (int)(__float_as_uint(x) >> 23);
+  return __uint_as_float((uint32_t)(254 - (e < 1 ? 1 : (e < 253 ? e : 253))) << 23);
 }
 
 // The first v_tiles workgroups take tiles of values, the others a token each.
 // NORM: y = x * (sum x^2 / D + eps)^(-1/2) * w for every head first, over the 4 or 8
-// lanes that hold it, in fp32; nothing is rounded between norm and turn.  8192 tokens of 32 and 8
+// lanes that hold it, in fp32; nothing is rounded between norm and turn.  bf16 reaches 2^128, its squares 2^256: a
+// head whose mean square is far from 1 is scaled by a power of two, with eps, and squared again, so that nothing
+// leaves fp32 (scaled always, 8192 tokens take 39.7 us, so 38.5).  8192 tokens of 32 and 8
 // heads of 128 take 41.6 us with norms and 40 without, 202 MB at the rate of a copy either way.
 template <bool NORM>
 __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const AppendArgs a) {
@@ -196,10 +213,23 @@ __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const App
     load8(src + o1, y);
     if (NORM && (key ? l.k_weight : l.q_weight)) {
       const float* const weight = s.turn.weight[key ? 1 : 0];
-      float sum = 0.f;
+      auto mean_square = [&](float eps) {
+        float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += x[e] * x[e], sum += y[e] * y[e];
-      const float r = 1.f / sqrtf(head_sum(sum, per_head) / D + l.eps);
+        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(y[e], y[e], __builtin_fmaf(x[e], x[e], sum));
+        return over_head(sum, per_head, [](float p, float q) { return p + q; }) / D + eps;
+      };
+      float mean = mean_square(l.eps);
+      if (!(mean >= 0x1p-40f && mean <= 0x1p40f)) {   // a head's lanes agree
+        float top = a.root_eps;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf(x[e]), fabsf(y[e])));
+        const float scale = to_one(over_head(top, per_head, [](float p, float q) { return fmaxf(p, q); }));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= scale, y[e] *= scale;
+        mean = mean_square(l.eps * scale * scale);
+      }
+      const float r = 1.f / sqrtf(mean);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] *= r * weight[o0 + e], y[e] *= r * weight[o1 + e];
     }
@@ -210,15 +240,15 @@ __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const App
           const float c0 = s_cos[8 * c + e], s0 = s_sin[8 * c + e];
           const float c1 = s_cos[8 * c + 4 + e], s1 = s_sin[8 * c + 4 + e];
           const float p = x[2 * e], q = x[2 * e + 1], r = y[2 * e], u = y[2 * e + 1];
-          x[2 * e] = p * c0 - q * s0, x[2 * e + 1] = q * c0 + p * s0;
-          y[2 * e] = r * c1 - u * s1, y[2 * e + 1] = u * c1 + r * s1;
+          turn(p, q, c0, s0, x[2 * e], x[2 * e + 1]);
+          turn(r, u, c1, s1, y[2 * e], y[2 * e + 1]);
         }
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float cs = s_cos[8 * c + e], sn = s_sin[8 * c + e];
           const float p = x[e], q = y[e];
-          x[e] = p * cs - q * sn, y[e] = q * cs + p * sn;
+          turn(p, q, cs, sn, x[e], y[e]);
         }
       }
     }
@@ -249,7 +279,7 @@ __global__ __launch_bounds__(kAppendThreads) void rotary_append_kernel(const App
 
 hipError_t launch_rotary_append(const CacheDims& d, const AppendLaunch& l, hipStream_t st) {
   if (l.num_tokens == 0) return hipSuccess;
-  AppendArgs a{l, d.Hq, d.Hkv, d.D, (long long)d.num_pages * kPage, d.v_layout != 0, 0};
+  AppendArgs a{l, d.Hq, d.Hkv, d.D, (long long)d.num_pages * kPage, d.v_layout != 0, 0, std::sqrt(l.eps)};
   // Tiles pay where tokens lie in runs, which the host does not know; by their number a
   // prompt's chunk and a decode step's tokens, which lie in a page each, are told apart.
   // 32/8 heads, D = 128, without tiles and with: 512 tokens of a prompt 8.1 and 4.7 us, 2048

@@ -200,3 +200,32 @@ def test_graph_and_stream():
         got, kp = out.clone(), pools[0].clone()
         want = ca.rotary_append(c, r, q, k, v, pos, slots, pools)
         assert torch.equal(got, want) and torch.equal(kp, pools[0])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", [60, 61, 62, 63, 64, 100, 126, 127, -62, -63, -64, -75, -80, -100, -126, -130, -133])
+def test_heads_of_any_size(D, power):
+    """Squares and their sums stay in range wherever the elements are: mean squares on both sides of 2^121 and
+    2^127, heads of the largest bf16 and of subnormal ones, with and without eps."""
+    rng = np.random.default_rng(1000 + D + power)
+    x = np.full((12, 8, D), np.float32(2.0) ** power)
+    x[4:] *= rng.choice(np.float32([1, -1]), (8, 8, D))
+    if power > -126:
+        x[8:] *= rng.choice(np.float32([1, 2.0 ** -20, 2.0 ** -5]), (4, 8, D))
+        x[8:, :, 5] = np.float32(2.0) ** power * np.float32(1.5)
+    bits = synth.bf16_round(x)
+    assert np.array_equal(synth.bf16_bits_to_f32(bits), x)
+    for eps in (0.0, 1e-6, 1e-38):
+        _case(rng, 12, 4, 2, D, x=bits, eps=eps)
+    _case(rng, 12, 4, 2, D, x=bits, eps=0.0, wide=True, offset=1, rot=0)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_one_large_element(D):
+    """A head whose largest element is far from the others, at the ends of what bf16 holds."""
+    rng = np.random.default_rng(D)
+    for large, small in ((3.3e38, 1e30), (1e20, 1e-20), (1e-20, 1e-38), (2.0 ** -100, 2.0 ** -133)):
+        x = np.full((6, 8, D), np.float32(small))
+        x[:, :, 7] = np.float32(large)
+        for eps in (0.0, 1e-6):
+            _case(rng, 6, 4, 2, D, x=synth.bf16_round(x), eps=eps)
