@@ -42,6 +42,7 @@ constexpr int kPairs = 3;                     // of those; the other two waves a
 constexpr int kCost = 4;                      // of a page that memory bounds, see page_cost
 constexpr int kManyPages = 4 * kGroups;       // from so many on, pages count by their cost
 constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = 1 << 23;            // of a launch: one has fewer than 2^32 threads
 constexpr float kSlack = 8.f;                 // log2 of the largest weight
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -802,15 +803,15 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_kernel(const PrefixArgs a)
 // A query row's parts: of its share's items and of its own, each whole or in the pieces of several
 // workgroups.  A thread takes 4 dimensions of every lots-th piece.
 template <int D>
-__global__ __launch_bounds__(kJoinThreads) void prefix_join_kernel(const PrefixArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void prefix_join_kernel(const PrefixArgs a, int first) {
   constexpr int kEach = D / 4, kLots = kJoinThreads / kEach;
   __shared__ float4 s_o[kJoinThreads];
   __shared__ float2 s_ml[kLots];
   const int tid = threadIdx.x, lot = tid / kEach, d = 4 * (tid % kEach);
-  const int b = blockIdx.x / a.Hq, h = blockIdx.x - b * a.Hq, kvh = h / a.G, head = h - kvh * a.G;
+  const int at_row = first + blockIdx.x, b = at_row / a.Hq, h = at_row - b * a.Hq, kvh = h / a.G, head = h - kvh * a.G;
   const int4 p0 = a.plan[3 * b], p1 = a.plan[3 * b + 1], p2 = a.plan[3 * b + 2];
   const Where at = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w, p2.x, p2.y};
-  const long long out_row = (long long)b * a.Hq + h;
+  const long long out_row = at_row;
   float top = -INFINITY, all = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float2 ml, const float4& o) {
@@ -866,10 +867,14 @@ int slot_rows_of(const CacheDims& d) {
 template <int D, bool VT>
 hipError_t launch(const PrefixArgs& a, hipStream_t st) {
   prefix_kernel<D, VT><<<kGroups, kThreads, 0, st>>>(a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  prefix_join_kernel<D><<<a.B * a.Hq, kJoinThreads, 0, st>>>(a);
-  return hipGetLastError();
+  hipError_t e = hipGetLastError();
+  const int rows = a.B * a.Hq;   // below 2^28
+  for (int first = 0; e == hipSuccess && first < rows; first += kJoinRows) {
+    const int n = rows - first < kJoinRows ? rows - first : kJoinRows;
+    prefix_join_kernel<D><<<n, kJoinThreads, 0, st>>>(a, first);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 }  // namespace

@@ -373,3 +373,28 @@ def test_keys_without_weight_add_nothing(D, Hq, members, layout):
             err = np.abs(bf16_host_f64(out[b]) - want)
             assert (err <= BF16_HALF * np.abs(want) + (2.0 ** -16 + 2.0 ** -19) * mass).all(), (score, b, err.max())
             assert np.abs(lse[b].cpu().numpy() - np.log(there.sum())).max() <= 2.0 ** -19 * np.log(there.sum())
+
+
+def test_as_many_rows_as_a_launch_has_workgroups():
+    """2^24 query rows and more: the join's workgroups of 256 threads are more than one launch takes.  A request
+    with one key gets its value exactly, and lse 0 from a query of zeros."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(14)
+    pages, D = 500, 64
+    for B, Hq, Hkv in ((2048, 8192, 64), (2047, 257 * 32, 32)):
+        c = ca.Cache(B, Hq, Hkv, D, 1, pages)
+        kp, vp = (torch.randn((pages, 64, D), generator=g, device=DEV, dtype=torch.bfloat16) for _ in "kv")
+        pt = torch.randint(0, pages, (B, Hkv, 1), generator=g, device=DEV, dtype=torch.int32)
+        lens = (torch.arange(B, device=DEV) % 3 > 0).to(torch.int32)
+        q = torch.zeros(B, Hq, D, device=DEV, dtype=torch.bfloat16)
+        out, lse = torch.full_like(q, 9.0), torch.full((B, Hq), 7.0, device=DEV)
+        none = torch.empty(0, dtype=torch.int32, device=DEV)
+        ca.sharing.prefix_decode_attention(c, q, (kp, vp), pt, lens, torch.full_like(lens, -1), none, 0.1, out=out, lse=lse)
+        torch.cuda.synchronize()
+        for b in range(0, B, 256):
+            some = slice(b, b + 256)
+            want = vp[pt[some, :, 0].long(), 0] * lens[some, None, None].to(torch.bfloat16)
+            got = out[some].view(-1, Hkv, Hq // Hkv, D)
+            assert (got == want[:, :, None]).all()
+            assert (lse[some] == torch.where(lens[some] > 0, 0.0, -float("inf"))[:, None]).all()
+        del q, out, lse
