@@ -636,7 +636,8 @@ ca_status ca_compact_pages(const ca_cache* c, const int32_t* seq_len, const int3
 /* 6c. ca_decode_attention for requests that share prefixes, each read once for all
  *    of its requests.  share int32 [B]: the share of request b, none where it is outside
  *    0 .. num_shares - 1; share_len int32 [num_shares]: the tokens that the
- *    requests of a share have in common, of which the whole pages count:
+ *    requests of a share have in common (their length at the fork: not the tokens
+ *    that each has added since), of which the whole pages count:
  *    P = share_len / 64 (at most max_kv_blocks).  A request of the share with
  *    kv_len >= 64 P is a member; one that is shorter (an idle row) is taken by itself.
  *    The keys of blocks 0 .. P - 1 are read through the table row of the

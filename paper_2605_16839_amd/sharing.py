@@ -9,6 +9,8 @@ requests that may share pages end here (``parent[b] = -1``), not by ``release_pa
     state = dict(seq_len=seq_len, page_table=page_table, page_shares=shares,
                  free_pages=free_pages, free_count=free_count)
     ca.sharing.fork_requests(cache, parent, **state, kv_pool=pools, bufs=dict(state))   # in place
+    share_len = seq_len[:1].clone()   # what all have in common: as it is at the fork
+    # a step's tokens: assign_slots, rotary_append
     out, _ = ca.sharing.prefix_decode_attention(cache, q, pools, page_table, seq_len, share,
                                                 share_len, sm_scale)
 
@@ -126,7 +128,9 @@ def prefix_decode_attention(c: Cache, q: torch.Tensor, kv_pool: Tuple[torch.Tens
                             ws: Optional[torch.Tensor] = None, stream=None):
     """``decode_attention`` for requests that share prefixes: share[b] names the share of request b (-1:
     none), whose first share_len[share[b]] tokens it has in common with the share's others; their whole
-    pages are read once for all of them.  Returns (out bf16, lse fp32 or None)."""
+    pages are read once for all of them.  After a fork that is the length at the fork: tokens that a
+    request adds later are its own, and a share_len that counts them reads the first member's for all.
+    Returns (out bf16, lse fp32 or None)."""
     if stream is not None:
         return _on(stream, prefix_decode_attention, locals())
     index, st = _here(q)
