@@ -590,7 +590,9 @@ ca_status ca_norm_rotary_append(const ca_cache* c, const ca_rotary* r, const ca_
  *      - pages that no request holds any more go behind the free ones, by ascending id.
  *    Lengths out of range (below 0, past max_kv_blocks) count as 0.  Entries that
  *    are no page are handed on as they are, and a free page that is none is given away
- *    but not written to.  free_capacity must be at least num_pages.
+ *    but not written to.  With page_shares below 0, which no call leaves, the free list and
+ *    its count may be wrong; nothing is written out of range.  free_capacity must be at
+ *    least num_pages.
  *    Written: seq_len_out [B], page_table_out (the blocks that the requests
  *    then have; entries behind them are left alone), page_shares_out,
  *    free_pages_out (the free ones) and free_count_out.  Each may be its input,

@@ -271,7 +271,8 @@ __global__ __launch_bounds__(kRowThreads) void fork_free_kernel(const ForkArgs a
       const int place = at + block_sum(gone ? 1 : 0, s_part, &n) - 1;
       if (gone) {
         l.page_shares_out[p] = 0;
-        if (place < l.free_capacity) l.free_pages_out[place] = (int)p;
+        // (below 0 where a count was below 0 before: such a page may be listed and not counted)
+        if (place >= 0 && place < l.free_capacity) l.free_pages_out[place] = (int)p;
       }
       at += n;
     }
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(kRowThreads) void fork_free_kernel(const ForkArgs a
     }
   if (c == 0 && tid == 0) {
     const long long n = (long long)left + all;
-    l.free_count_out[0] = (int)(n < l.free_capacity ? n : l.free_capacity);
+    l.free_count_out[0] = (int)(n < 0 ? 0 : (n < l.free_capacity ? n : l.free_capacity));
   }
 }
 

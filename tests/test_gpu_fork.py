@@ -291,3 +291,36 @@ def test_more_rows_than_lds_holds(in_place):
 def test_compact_of_small_and_larger_pools(pages, in_place):
     """Sizes at which the last word of a map in LDS ends, and on both sides of the largest pool with one."""
     test_compact(4, 2 if pages > 40 else 1, 2 if pages < 40 else 20, pages, True, 64, in_place)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_counts_below_zero_write_nothing_out_of_range(in_place):
+    """A count of -1 in one chunk of the ids takes a page off the places of the next chunk's: with no free page
+    before, its first would be listed at -1.  Every output lies between guards."""
+    rng = np.random.default_rng(21)
+    B, most, pages = 8, 2, 700
+    c = ca.Cache(B, 1, 1, 64, most, pages)
+    pools = _pools(rng, pages, 64)
+    shapes = dict(seq_len=(B,), page_table=(B, 1, most), page_shares=(pages,), free_pages=(pages,), free_count=(1,))
+    for case in range(20):
+        lens = np.array([64, 0, 64, 0, 128, 100, 0, 64])
+        table, shares = np.full((B, 1, most), -1), np.zeros(pages, dtype=np.int64)
+        table[0, 0, 0], table[2, 0, 0], table[4, 0], table[5, 0], table[7, 0, 0] = 3, 300, (10, 520), (11, 521), 690
+        parent = np.array([0, 0, -1, 3, 4, 4, 0, -1])
+        shares[3] = -1
+        if case:
+            shares = rng.integers(-3, 2, pages)
+            parent = rng.integers(-1, B, B)
+        free = [] if case % 2 == 0 else [600, 601]
+        guarded = {n: torch.full((int(np.prod(s)) + 128,), -77, dtype=torch.int32, device=DEV) for n, s in shapes.items()}
+        bufs = {n: guarded[n][64:64 + int(np.prod(s))].view(s) for n, s in shapes.items()}
+        d = _devs(lens, table, shares, free, pages)
+        if in_place:
+            for n in NAMES:
+                bufs[n].copy_(d[n])
+            d = dict(bufs)
+        ca.sharing.fork_requests(c, i32_dev(parent), *[d[n] for n in NAMES], pools, bufs=bufs)
+        torch.cuda.synchronize()
+        for n, t in guarded.items():
+            assert (t[:64] == -77).all() and (t[-64:] == -77).all(), (case, n)
+        assert 0 <= int(bufs["free_count"]) <= pages
