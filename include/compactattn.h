@@ -592,13 +592,14 @@ ca_status ca_norm_rotary_append(const ca_cache* c, const ca_rotary* r, const ca_
  *    are no page are handed on as they are, and a free page that is none is given away
  *    but not written to.  With page_shares below 0, which no call leaves, the free list and
  *    its count may be wrong; nothing is written out of range.  free_capacity must be at
- *    least num_pages.
+ *    least num_pages.  B < 2^24 (else CA_ERR_UNSUPPORTED); every row goes through all
+ *    requests for its forks, so the time of very many grows with B x B.
  *    Written: seq_len_out [B], page_table_out (the blocks that the requests
  *    then have; entries behind them are left alone), page_shares_out,
  *    free_pages_out (the free ones) and free_count_out.  Each may be its input,
  *    and a page table in place has only the rows that change written; other
  *    buffers may not overlap.  The pools have the copies written.
- *    Workspace: ca_fork_workspace_bytes(c) bytes, 16-byte aligned, whatever it
+ *    Workspace: ca_fork_workspace_bytes(c) bytes (0 if refused), 16-byte aligned, whatever it
  *    holds; calls that may overlap must not share one.
  *
  * 6b. ca_compact_pages: moves pages so that the U pages in use (all that are not in

@@ -446,6 +446,15 @@ ca_status need_workspace(const char* what, size_t need, const void* ws, size_t w
   return ok();
 }
 
+// The cache of a call that forks requests.
+ca_status check_fork(const ca_cache* c, ca::CacheDims* d) {
+  const ca_status s = check_cache(c, 0, d);
+  if (s != CA_OK) return s;
+  if (d->B > ca::kForkRequests)
+    return fail(CA_ERR_UNSUPPORTED, "batch %d > %d", d->B, ca::kForkRequests);
+  return ok();
+}
+
 // The cache of a call whose requests share prefixes.
 ca_status check_prefix(const ca_cache* c, int32_t num_shares, ca::CacheDims* d) {
   const ca_status s = check_cache(c, 0, d);
@@ -1149,7 +1158,7 @@ ca_status ca_decode_attention(const ca_cache* c, const uint16_t* q, const uint16
 
 size_t ca_fork_workspace_bytes(const ca_cache* c) {
   ca::CacheDims d;
-  return check_cache(c, 0, &d) == CA_OK ? ca::fork_ws_bytes(d) : 0;
+  return check_fork(c, &d) == CA_OK ? ca::fork_ws_bytes(d) : 0;
 }
 
 ca_status ca_fork_requests(const ca_cache* c, const int32_t* parent, const int32_t* keep_len,
@@ -1160,7 +1169,7 @@ ca_status ca_fork_requests(const ca_cache* c, const int32_t* parent, const int32
                            int32_t* page_shares_out, int32_t* free_pages_out,
                            int32_t* free_count_out, void* ws, size_t ws_bytes, void* stream) {
   ca::CacheDims d;
-  ca_status s = check_cache(c, 0, &d);
+  ca_status s = check_fork(c, &d);
   if (s != CA_OK) return s;
   if (!parent || !seq_len || !page_table || !page_shares || !free_pages || !free_count ||
       !k_pool || !v_pool || !seq_len_out || !page_table_out || !page_shares_out ||

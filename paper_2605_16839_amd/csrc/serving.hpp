@@ -69,6 +69,8 @@ struct DecodeLaunch {
 size_t decode_ws_bytes(const CacheDims& d);
 hipError_t launch_decode(const CacheDims& d, const DecodeLaunch& a, hipStream_t st);
 
+constexpr int kForkRequests = (1 << 24) - 1;   // at most: a launch has fewer than 2^32 threads, 256 for a request
+
 struct ForkLaunch {
   const int32_t* parent;
   const int32_t* keep_len;     // nullptr: all tokens

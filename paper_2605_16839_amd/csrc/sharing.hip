@@ -517,6 +517,7 @@ int chunk_of(int num_pages) {   // ids of a chunk: whole rounds of a workgroup's
 }
 size_t aligned16(size_t n) { return (n + 15) / 16 * 16; }
 static_assert(kChunks == kRowThreads, "a thread for every chunk");
+static_assert((long long)kForkRequests * kRowThreads <= UINT32_MAX, "workgroups of fork_rows_kernel");
 
 }  // namespace
 

@@ -189,3 +189,12 @@ def test_a_call_runs_under_its_stream(monkeypatch, name):
     called.clear()
     fn(*args, *rest, mark)
     assert called == [mark]
+
+
+def test_fork_refuses_more_rows_than_a_launch_has_workgroups(lib):
+    """Its second launch has 256 threads for every row, and a launch fewer than 2^32."""
+    most = dict(num_q_heads=1, num_kv_heads=1, max_kv_blocks=1)
+    for batch, code in ((1 << 24, "CA_ERR_UNSUPPORTED"), ((1 << 24) - 1, "CA_ERR_WORKSPACE")):
+        c = _cache(batch=batch, **most)
+        assert _call(lib, lib.ca_fork_requests, FORK, c.ref, ws=None) == code
+        assert (lib.ca_fork_workspace_bytes(c.ref) == 0) == (code == "CA_ERR_UNSUPPORTED")
