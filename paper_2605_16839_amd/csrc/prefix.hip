@@ -14,12 +14,16 @@
 // is read from LDS by all waves, for 16 or 32 rows each.
 //
 // What bounds it (32 and 8 heads of 128): behind one prefix of 126976 tokens, 128 requests with up to 4096
-// of their own, 482 us, 556 TFLOP/s, the weights' VALU work: of a SIMD's cycles MFMA has 40% and VALU
-// instructions, with the exponentials' four rounds, about 70%; LDS 15%.  Taking turns at MFMA and VALU between a
-// SIMD's two waves, and scores a page ahead of their weights, measured the same, row sums by MFMA 6% more.
+// of their own take 490 us from graphs (488 to 497; 540 in the first launches after a pause), 547 TFLOP/s.  No
+// unit is full: of a SIMD's cycles MFMA has 39%, the other VALU instructions 46% (an exponential two turns), LDS
+// 16%; waves wait 30% of their time for a barrier or for loads, and 30% for their turn.  A wave makes a page's weights before its
+// first MFMA of V, and all meet at a barrier every page, so the two kinds of work mostly come one after
+// the other.  Left to the compiler's order, scores half a page ahead of their weights took 3% more, half of the
+// waves half a page behind the others the same; row sums by MFMA 6% more.
 // Own pages and short prefixes are bound by memory: 96 requests, 6 prefixes of 1500 to 16000 tokens,
-// up to 6000 of their own, 161 us, 4.6 TB/s.  The smallest calls, 15 us, are two launches and the walk from
-// lengths to pages.
+// up to 6000 of their own, 163 us, 4.6 TB/s.  The smallest calls, 14.5 us, are two launches, the plan and the walk
+// from lengths to pages.  Where few requests share little, ca_decode_attention is faster: 8.8 us for 3 requests
+// behind 700 tokens; 8 requests (8 KV heads of 128) break even at 3000 shared tokens, 64 at 1200.
 #include <type_traits>
 
 #pragma clang diagnostic ignored "-Winline-asm"   // page_to_lds names m0, which is reserved, as what it changes
@@ -40,7 +44,10 @@ constexpr int kQueue = 128;                   // pages that are looked up togeth
 constexpr int kPairRows = 8;                  // rows of a request's item that a pair of waves takes
 constexpr int kPairs = 3;                     // of those; the other two waves ask for pages then
 constexpr int kCost = 4;                      // of a page that memory bounds, see page_cost
-constexpr int kManyPages = 4 * kGroups;       // from so many on, pages count by their cost
+// From so many pages on they count by their cost.  Of 22 calls of 4 to 128 requests, with 32 kGroups 64 requests
+// behind 16000 tokens (8 KV heads) take 120 us instead of 83 and five calls 6 to 8% more; with kGroups 64 behind 2000
+// (2 KV heads) take 29 instead of 35; the others are within 4%.
+constexpr int kManyPages = 4 * kGroups;
 constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = 1 << 23;            // of a launch: one has fewer than 2^32 threads
 constexpr float kSlack = 8.f;                 // log2 of the largest weight
@@ -76,8 +83,12 @@ __device__ __forceinline__ int rows_of_tile(long long rows) {
   return tiles < 2 ? kTile : (int)(((rows + tiles - 1) / tiles + 31) / 32 * 32);
 }
 // What a page costs with so many rows to a tile, in units of which a page of up to 32 rows, that memory
-// bounds, has kCost.  Measured of a page: 1.2 us (8 rows), 1.5 (56), 2.2 (128), 3.4 (256).  These
-// costs against 4, 4, 6 and 7, a step before: 168 us and 188 for the 96 requests above, 528 and 537 for the 128.
+// bounds, has kCost.  Measured of a page of 128 dimensions: 1.2 us (8 rows), 1.5 (56), 2.2 (128), 3.4 (256),
+// or 4, 5, 7.3 and 11.3.  Against costs of 4, 4, 6 and 7: the 96 requests above 165 us and 189, the 128 488 and 493, 16
+// behind a document (128 rows) 57.6 and 57.0, shares of 128 rows beside as many own pages 141 and 147, with four times the own pages
+// 241 and 268.  128 rows have 5 and not 7 for calls of little else: with 7 the document takes 61.2, but the two others
+// 135 and 218, and the 96 requests 153.  Pages of 64 dimensions have the same costs: 196 us and 214 with many own
+// pages, 410 and 372 for the 128.
 __device__ __forceinline__ int page_cost(long long rows) {
   const long long all = rows < kTile ? rows : rows_of_tile(rows);
   return all <= 32 ? kCost : all <= 128 ? 5 : (all <= 192 ? 9 : 11);

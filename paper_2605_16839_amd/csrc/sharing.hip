@@ -15,10 +15,11 @@
 // below U; both ranks are prefix sums over the ids.  Small pools: FreeMap.
 //
 // What bounds them: latency, launch by launch; with many pages to copy HBM, read and write.  A prompt of
-// 32741 tokens (8 KV heads of 128) for 64 requests: 15.9 us a call, of which plan 4.3 (one workgroup, its
-// barriers), rows 7.1 (four loads that wait for each other, then 504 pages copied), free 2.8; compaction
-// of a pool of 81K pages, half of them in use and 20K of those moved, 286 us, of which the moves 260: 1.33 GB
-// at 5 TB/s.
+// 32741 tokens (8 KV heads of 128) for 64 requests: 15.7 us a call, of which plan 4.3 (one workgroup, its
+// barriers), rows 7.4 (four loads that wait for each other, then 504 pages copied), free 3.1; in place 2 us more
+// (rows are written twice), 16 prompts of 4 beams 17.0 and 5 more.  Compaction of a pool of 81K pages, half of them in use
+// and 20K of those moved, 285 us, of which the moves 268: 1.33 GB at 5 TB/s; in place the same, a small pool
+// 2 us more for its second launch.
 #include "common.hpp"
 #include "serving.hpp"
 

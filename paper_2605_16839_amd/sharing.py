@@ -130,6 +130,8 @@ def prefix_decode_attention(c: Cache, q: torch.Tensor, kv_pool: Tuple[torch.Tens
     none), whose first share_len[share[b]] tokens it has in common with the share's others; their whole
     pages are read once for all of them.  After a fork that is the length at the fork: tokens that a
     request adds later are its own, and a share_len that counts them reads the first member's for all.
+    Where the prefixes read again for every request would be less than some 100 to 250 MB,
+    ``decode_attention`` is faster.
     Returns (out bf16, lse fp32 or None)."""
     if stream is not None:
         return _on(stream, prefix_decode_attention, locals())
