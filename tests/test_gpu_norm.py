@@ -229,3 +229,15 @@ def test_one_large_element(D):
         x[:, :, 7] = np.float32(large)
         for eps in (0.0, 1e-6):
             _case(rng, 6, 4, 2, D, x=synth.bf16_round(x), eps=eps)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_heads_of_all_sizes_side_by_side(D):
+    """Scaled and unscaled heads in one wave, in any order."""
+    rng = np.random.default_rng(40 + D)
+    for Hq, Hkv in ((4, 2), (21, 7), (33, 1)):
+        heads = Hq + 2 * Hkv
+        x = rng.standard_normal((30, heads, D)).astype(np.float32)
+        x *= np.float32(2.0) ** rng.choice([-120, -64, -20, -19, 0, 0, 0, 19, 21, 62, 120], (30, heads, 1)).astype(np.float32)
+        _case(rng, 30, Hq, Hkv, D, x=synth.bf16_round(x), eps=0.0)
+        _case(rng, 30, Hq, Hkv, D, x=synth.bf16_round(x), eps=1e-6, wide=True, interleaved=True)
